@@ -6,13 +6,11 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdarg>
 #include <new>
-#include <cstdio>
 #include <cstring>
 #include <mutex>
 
-#include "aug_internal.h"
+#include "api_common.h"
 
 namespace aug {
 
@@ -49,6 +47,14 @@ void DeviceBuffer::release() {
 namespace {
 
 using aug::DeviceBuffer;
+using aug::enter;
+using aug::fail;
+using aug::fail_hip;
+using aug::grow;
+using aug::mark;
+using aug::packing_launched;
+using aug::ring_bytes;
+using aug::ring_reserve;
 
 // ---- the static scratch array of aug_vtlp_mel_batch_static ----
 // Device memory that is part of the library's code object: every GPU that loads the library holds its own
@@ -74,36 +80,6 @@ struct ScratchLayout {
     static constexpr size_t end = mel_tab + align256(mel_tab_bytes);
 };
 static_assert(ScratchLayout::end <= AUG_STATIC_SCRATCH_BYTES, "the tables fit the static array");
-
-int fail(aug_ctx* ctx, int code, const char* fmt, ...) {
-    if (ctx) {
-        char msg[512];
-        va_list ap;
-        va_start(ap, fmt);
-        vsnprintf(msg, sizeof msg, fmt, ap);
-        va_end(ap);
-        ctx->last_error = msg;
-    }
-    return code;
-}
-
-int fail_hip(aug_ctx* ctx, hipError_t e, const char* what) {
-    (void)hipGetLastError();
-    if (e == hipErrorOutOfMemory) return fail(ctx, AUG_ERR_NOMEM, "%s: out of device memory", what);
-    return fail(ctx, AUG_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-}
-
-#define AUG_HIP(expr, what)                                        \
-    do {                                                           \
-        hipError_t e__ = (expr);                                   \
-        if (e__ != hipSuccess) return fail_hip(ctx, e__, what);    \
-    } while (0)
-
-#define AUG_TRY(expr)                                              \
-    do {                                                           \
-        int rc__ = (expr);                                         \
-        if (rc__ != AUG_OK) return rc__;                           \
-    } while (0)
 
 int check_offsets(aug_ctx* ctx, int n_utt, const int64_t* offsets) {
     if (n_utt < 0) return fail(ctx, AUG_ERR_INVALID_ARG, "n_utt is negative");
@@ -154,43 +130,6 @@ int check_frame_offsets(aug_ctx* ctx, int n_utt, const int64_t* offsets, const i
     return AUG_OK;
 }
 
-// Grow one of the context's device buffers.  Growing frees the old allocation (which waits for the work
-// that uses it) and allocates: neither may happen while the stream is being captured into a graph.
-int grow(aug_ctx* ctx, DeviceBuffer& b, size_t bytes, const char* what) {
-    if (bytes <= b.bytes) return AUG_OK;
-    hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
-    if (hipStreamIsCapturing(ctx->stream, &st) != hipSuccess) (void)hipGetLastError();
-    if (st != hipStreamCaptureStatusNone)
-        return fail(ctx, AUG_ERR_UNSUPPORTED, "%s would have to grow while the stream is being captured: "
-                    "run the same call once before capturing it", what);
-    hipError_t e = b.reserve(bytes);
-    if (e != hipSuccess) return fail_hip(ctx, e, what);
-    return AUG_OK;
-}
-
-// Bytes of a staging slot for n_utt + 1 = n entries: two int64 and two int arrays.
-size_t ring_bytes(size_t n) { return n * (2 * sizeof(int64_t) + 2 * sizeof(int)); }
-
-// Pinned staging slots of at least `bytes` each, with their events.
-int ring_reserve(aug_ctx* ctx, size_t bytes) {
-    aug::HostRing& r = ctx->ring;
-    if (bytes <= r.bytes) return AUG_OK;
-    AUG_HIP(hipStreamSynchronize(ctx->stream), "stream synchronize");       // kernels still read the old slots
-    if (r.host) {
-        AUG_HIP(hipHostFree(r.host), "staging free");
-        r.host = nullptr;
-    }
-    r.bytes = 0;
-    const size_t want = (bytes + bytes / 4 + 4095) & ~(size_t)4095;
-    AUG_HIP(hipHostMalloc(reinterpret_cast<void**>(&r.host), want * aug::HostRing::kSlots, hipHostMallocDefault),
-            "pinned staging buffer");
-    AUG_HIP(hipHostGetDevicePointer(reinterpret_cast<void**>(&r.device), r.host, 0), "pinned staging address");
-    for (hipEvent_t& e : r.done)
-        if (!e) AUG_HIP(hipEventCreateWithFlags(&e, hipEventDisableTiming), "staging event");
-    r.bytes = want;
-    return AUG_OK;
-}
-
 // Write a batch's arrays into the next staging slot and point `pa` at them, without waiting for the stream; the caller
 // launches the packing (alone, or with the front end's set-up) and then calls packing_launched.  conv_block > 0 and
 // frame_offsets (with pa.shares) ask for that table; upload_offsets is false where the device already holds these offsets.  The
@@ -233,16 +172,6 @@ int stage_packing(aug_ctx* ctx, aug::PackArgs& pa, const int64_t* offsets, bool 
         first[pa.n_utt] = at;
         pa.conv_first = reinterpret_cast<const int*>(d + 2 * i64);
     }
-    return AUG_OK;
-}
-
-// The kernel that reads the current staging slot has been enqueued.
-int packing_launched(aug_ctx* ctx) {
-    aug::HostRing& r = ctx->ring;
-    const int i = r.next, e = i / aug::HostRing::kPerEvent;
-    if (i % aug::HostRing::kPerEvent == aug::HostRing::kPerEvent - 1)
-        AUG_HIP(hipEventRecord(r.done[e], ctx->stream), "staging event record");
-    r.next = (i + 1) % aug::HostRing::kSlots;
     return AUG_OK;
 }
 
@@ -366,20 +295,6 @@ int ensure_conv_table(aug_ctx* ctx, int n, const float2** out) {
         AUG_HIP(aug::launch_conv_table(ctx->stream, n, b.as<float2>()), "convolution tables kernel");
     }
     *out = b.as<float2>();
-    return AUG_OK;
-}
-
-// Record an event that closes stage `stage` (or opens a timed span when stage < 0).
-int mark(aug_ctx* ctx, int stage) {
-    if (!ctx->profiling) return AUG_OK;
-    hipEvent_t ev;
-    AUG_HIP(hipEventCreate(&ev), "event create");
-    hipError_t e = hipEventRecord(ev, ctx->stream);
-    if (e != hipSuccess) {
-        (void)hipEventDestroy(ev);
-        return fail_hip(ctx, e, "event record");
-    }
-    ctx->marks.emplace_back(ev, stage);
     return AUG_OK;
 }
 
@@ -600,13 +515,6 @@ int check_mix_args(aug_ctx* ctx, int n_utt, int64_t total, int n_noise, const vo
     if (!speech && total > 0) return fail(ctx, AUG_ERR_INVALID_ARG, "speech is null");
     if (n_noise > 0 && ((!noise && total > 0) || (!snr_db && n_utt > 0)))
         return fail(ctx, AUG_ERR_INVALID_ARG, "noise or snr_db is null");
-    return AUG_OK;
-}
-
-int enter(aug_ctx* ctx) {
-    if (!ctx) return AUG_ERR_INVALID_ARG;
-    ctx->last_error.clear();
-    AUG_HIP(hipSetDevice(ctx->device), "set device");
     return AUG_OK;
 }
 
