@@ -320,6 +320,170 @@ int aug_pipeline_batch(aug_ctx* ctx, int n_utt, const int64_t* offsets, const fl
                        float* feats_out, float* rir_out, float* mixed_out, float* gains_out);
 
 /*
+ * ---- Operators on feature rows ----
+ *
+ * What a recogniser runs on the front end's rows before and between its matrix products: a root-mean-square norm
+ * with the residual's addition and an 8-bit output, a short causal convolution along time, and a selective scan of a
+ * state space.  Each has its gradients for training and, where it runs along time, a form for streams that get one
+ * row at a time.
+ *
+ * Conventions of this section, besides those above
+ *   - Activations have the type cfg->dtype; parameters, states of the scan, scales and gradients of parameters are
+ *     float.  Arithmetic, sums and states are 32 bits wide whatever the type; an output is rounded once, to nearest.
+ *   - aug_rows is a DEVICE matrix, row major: row r begins ld elements behind row r - 1 and ld is at least the width
+ *     of the call's rows, so that a column slice of a wider matrix needs no copy.  Elements behind a row's width
+ *     are neither read nor written.  An optional matrix or array is left out by a null pointer.  Addresses and ld need the
+ *     alignment of an element only.
+ *   - Sequences: row_offsets HOST int64 [n_seq+1], ascending, row_offsets[0] = 0: sequence i's rows begin at row
+ *     row_offsets[i] of every matrix.  row_lengths HOST int64 [n_seq] gives their numbers, at most row_offsets[i+1] -
+ *     row_offsets[i]; null: exactly that many.  frame_offsets of the front end are row_offsets; for its padded layout
+ *     give the frame counts as row_lengths.  Rows that belong to no sequence are neither read nor written.  Lengths of
+ *     0 are allowed; n_seq <= AUG_MAX_UTT and a sequence < 2^30 rows (AUG_ERR_UNSUPPORTED otherwise).
+ *   - Outputs must not overlap inputs or one another (AUG_ERR_INVALID_ARG) except where an argument says so.
+ *     Column slices of one matrix that share no column do not overlap.
+ *   - The same call gives the same bits: no sum is formed by floating-point atomics.
+ *   - The calls leave the host thread's current device as it was.
+ */
+enum { AUG_F32 = 0, AUG_BF16 = 1, AUG_F16 = 2 };      /* element types */
+
+typedef struct aug_rows {
+    void*   data;     /* DEVICE */
+    int64_t ld;       /* elements from one row to the next */
+} aug_rows;
+
+#define AUG_MAX_NORM_DIM 16384   /* columns of the norm */
+#define AUG_MAX_DIM 32768        /* channels of the convolution and of the scan */
+#define AUG_MAX_TAPS 8           /* taps of the short convolution */
+#define AUG_MAX_STATE 128        /* states per channel of the scan */
+
+typedef struct aug_norm_cfg {
+    int   dtype;      /* AUG_F32, AUG_BF16, AUG_F16 */
+    int   dim;        /* columns, 1..AUG_MAX_NORM_DIM */
+    float eps;        /* >= 0 */
+    int   q_block;    /* columns that share a scale of the 8-bit output: a power of two in 16..512, or 0 for the whole row */
+} aug_norm_cfg;
+
+/*
+ * Root-mean-square norm of rows, the residual added first:
+ *   s = x + residual,  y = s rstd weight,  rstd = 1 / sqrt(mean(s^2) + eps).
+ *
+ *   x          n_rows rows.  residual: as many, or null (s = x).
+ *   weight     DEVICE float [dim] or null (ones).
+ *   sum_out    s, or null.  May be x or residual.
+ *   y_out      y, or null.  May be x or residual (the same matrix, with the same ld).
+ *   q_out      y in 8 bits (OCP e4m3, one byte per element, ld in bytes), or null; then
+ *   scale_out  DEVICE float [n_rows][ceil(dim / q_block)], required with q_out: scale = max |y| / 448 over the
+ *              block's columns, q = y / scale rounded to nearest even, 0 where scale is 0.  y goes into both
+ *              unrounded.  A block that holds a NaN or an infinity has a scale that is none either.
+ *   rstd_out   DEVICE float [n_rows] or null: what the gradients need.
+ */
+int aug_rms_norm_batch(aug_ctx* ctx, int64_t n_rows, const aug_norm_cfg* cfg, const aug_rows* x, const aug_rows* residual,
+                       const float* weight, const aug_rows* sum_out, const aug_rows* y_out, const aug_rows* q_out,
+                       float* scale_out, float* rstd_out);
+
+/*
+ * Gradients of aug_rms_norm_batch by its sum s (which are those by x and by the residual) and by the weight:
+ *   dx = rstd (weight dy) - s rstd^3 mean(s weight dy) + dsum,   dweight = sum over rows of dy s rstd.
+ *
+ *   sum           s as the forward call gave it.     rstd   DEVICE float [n_rows] from the forward call.
+ *   dy            gradient by y.  (Through the 8-bit output the rounding counts as the identity.)
+ *   dsum          gradient by s from elsewhere (the residual stream), or null.
+ *   dx_out        may be dy, dsum or sum (the same matrix, with the same ld).  Null if not wanted.
+ *   dweight_out   DEVICE float [dim], overwritten, or null.
+ * cfg->eps and cfg->q_block are not used.
+ */
+int aug_rms_norm_backward_batch(aug_ctx* ctx, int64_t n_rows, const aug_norm_cfg* cfg, const aug_rows* sum, const float* weight,
+                                const float* rstd, const aug_rows* dy, const aug_rows* dsum, const aug_rows* dx_out,
+                                float* dweight_out);
+
+typedef struct aug_short_conv_cfg {
+    int dtype;
+    int dim;          /* channels, 1..AUG_MAX_DIM */
+    int taps;         /* 1..AUG_MAX_TAPS */
+    int silu;         /* not 0: y = p sigmoid(p); 0: y = p */
+} aug_short_conv_cfg;
+
+/*
+ * Short causal convolution along time, every channel with its own taps:
+ *   p[t][d] = bias[d] + sum_k weight[d][k] x[t - (taps-1) + k][d],   y = p or p sigmoid(p).
+ *
+ *   weight     DEVICE float [dim][taps].     bias  DEVICE float [dim] or null.
+ *   state_in   DEVICE dtype [n_seq][taps-1][dim]: the rows before each sequence's first, oldest first; null: zeros.
+ *   state_out  the same of the rows before what follows: the last taps-1 of state_in and the sequence's rows.  May be
+ *              state_in; null if not wanted.  (A sequence's rows may so be given in pieces.)
+ *   y_out      dim columns.
+ */
+int aug_short_conv_batch(aug_ctx* ctx, int n_seq, const int64_t* row_offsets, const int64_t* row_lengths,
+                         const aug_short_conv_cfg* cfg, const aug_rows* x, const float* weight, const float* bias,
+                         const void* state_in, void* state_out, const aug_rows* y_out);
+
+/*
+ * Its gradients, from dy: by x (dx_out), by the weight and by the bias (overwritten; each may be null).  state_in is
+ * what the forward call had and counts as a constant, and no gradient comes in by state_out: the truncated
+ * gradient of training in pieces.
+ */
+int aug_short_conv_backward_batch(aug_ctx* ctx, int n_seq, const int64_t* row_offsets, const int64_t* row_lengths,
+                                  const aug_short_conv_cfg* cfg, const aug_rows* x, const float* weight, const float* bias,
+                                  const void* state_in, const aug_rows* dy, const aug_rows* dx_out, float* dweight_out,
+                                  float* dbias_out);
+
+/* One row for each of n_seq streams: row i of x and y_out is stream i's.  Both states are required (state_in may be null with
+ * one tap, and state_out too); state_out may be state_in, y_out may be x (with the same ld). */
+int aug_short_conv_step(aug_ctx* ctx, int n_seq, const aug_short_conv_cfg* cfg, const aug_rows* x, const float* weight,
+                        const float* bias, const void* state_in, void* state_out, const aug_rows* y_out);
+
+typedef struct aug_scan_cfg {
+    int dtype;
+    int dim;          /* channels, 1..AUG_MAX_DIM */
+    int n_state;      /* states per channel, 1..AUG_MAX_STATE */
+    int n_group;      /* groups of dim / n_group channels that share b and c; divides dim */
+    int softplus;     /* not 0: step = ln(1 + exp(delta + delta_bias)); 0: step = delta + delta_bias */
+} aug_scan_cfg;
+
+/* What the scan reads. */
+typedef struct aug_scan_in {
+    aug_rows u;                 /* dim columns: the input */
+    aug_rows delta;             /* dim columns */
+    aug_rows b, c;              /* n_group * n_state columns: group g's begin at column g n_state */
+    aug_rows z;                 /* dim columns: the gate; z.data null: none */
+    const float* a;             /* DEVICE [dim][n_state]: rates, as a rule negative (a positive one lets states grow without bound) */
+    const float* skip;          /* DEVICE [dim] or null (zeros) */
+    const float* delta_bias;    /* DEVICE [dim] or null (zeros) */
+} aug_scan_in;
+
+/*
+ * Selective scan of a diagonal state space; channel d of group g, row t of a sequence, step = step[t][d]:
+ *   h[t][d][n] = exp(step a[d][n]) h[t-1][d][n] + step u[t][d] b[t][g][n]
+ *   p[t][d] = sum_n c[t][g][n] h[t][d][n] + skip[d] u[t][d],    y = p or, with a gate, p z sigmoid(z).
+ *
+ *   state_in   DEVICE float [n_seq][dim][n_state]: h before each sequence's first row; null: zeros.
+ *   state_out  h behind each sequence's last row (state_in's where it has none).  May be state_in; null if not wanted.
+ *   y_out      dim columns.
+ * Long sequences are cut into stretches that run side by side: a call with few sequences needs workspace for a state per stretch.
+ */
+int aug_scan_batch(aug_ctx* ctx, int n_seq, const int64_t* row_offsets, const int64_t* row_lengths, const aug_scan_cfg* cfg,
+                   const aug_scan_in* in, const float* state_in, float* state_out, const aug_rows* y_out);
+
+/* Where its gradients go; each may be null (a matrix by its data). */
+typedef struct aug_scan_grad {
+    aug_rows du, ddelta, db, dc, dz;        /* as u, delta, b, c, z; db and dc are sums over the group's channels */
+    float *da, *dskip, *ddelta_bias;        /* DEVICE float [dim][n_state], [dim], [dim], overwritten */
+} aug_scan_grad;
+
+/*
+ * Gradients of aug_scan_batch from dy.  in and state_in are what the forward call had; state_in counts as a constant and
+ * no gradient comes in by state_out.  No forward result is needed: states are computed anew.  dz must be null without a gate.
+ */
+int aug_scan_backward_batch(aug_ctx* ctx, int n_seq, const int64_t* row_offsets, const int64_t* row_lengths,
+                            const aug_scan_cfg* cfg, const aug_scan_in* in, const float* state_in, const aug_rows* dy,
+                            const aug_scan_grad* out);
+
+/* One row for each of n_seq streams: row i of the matrices is stream i's.  Both states are required; state_out may be
+ * state_in, and y_out may be u, delta or z (with the same ld). */
+int aug_scan_step(aug_ctx* ctx, int n_seq, const aug_scan_cfg* cfg, const aug_scan_in* in, const float* state_in,
+                  float* state_out, const aug_rows* y_out);
+
+/*
  * Per-stage device timing, for measurement (the stages are those of Sec. 2.3's path).
  * While enabled, every call records HIP events on the context's stream around each
  * stage's kernels.  aug_profile_read waits for the stream, adds up the elapsed
@@ -335,6 +499,9 @@ enum {
     AUG_STAGE_MEL,            /* STFT power, warped mel, power law */
     AUG_STAGE_OTHER,          /* clears and small tables */
     AUG_STAGE_VTLP,           /* waveform VTLP (aug_vtlp_resynth_batch) */
+    AUG_STAGE_NORM,           /* aug_rms_norm_* */
+    AUG_STAGE_SHORT_CONV,     /* aug_short_conv_* */
+    AUG_STAGE_SCAN,           /* aug_scan_* */
     AUG_N_STAGES
 };
 /*

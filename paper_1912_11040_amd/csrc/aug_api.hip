@@ -576,9 +576,11 @@ int aug_destroy(aug_ctx* ctx) {
     }
     DeviceBuffer* bufs[] = {&ctx->d_offsets, &ctx->d_frame_offsets, &ctx->d_conv_items, &ctx->d_conv_first,
                             &ctx->rir_items, &ctx->rir_ctrl, &ctx->visits, &ctx->rir, &ctx->rir_spec, &ctx->reverb, &ctx->energy, &ctx->first_tap, &ctx->vtlp_tab, &ctx->dct, &ctx->mel_tab, &ctx->mel_lanes,
-                            &ctx->window};
+                            &ctx->window, &ctx->rows.d_begin, &ctx->rows.d_end, &ctx->seq_ws};
     for (DeviceBuffer* b : bufs) b->release();
     for (DeviceBuffer& b : ctx->d_frame_items) b.release();
+    for (DeviceBuffer& b : ctx->rows.d_first) b.release();
+    for (DeviceBuffer& b : ctx->rows.d_items) b.release();
     for (DeviceBuffer& b : ctx->twiddle) b.release();
     for (DeviceBuffer& b : ctx->conv_tab) b.release();
     for (auto& m : ctx->marks) (void)hipEventDestroy(m.first);

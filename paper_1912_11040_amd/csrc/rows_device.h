@@ -1,0 +1,42 @@
+// Elements, rows and activations on the device, shared by the operators on feature rows.
+#pragma once
+
+#include "rows_internal.h"
+
+namespace aug {
+
+// Calls f with a value of the element type.
+template <class F> hipError_t with_type(int dtype, F f) {
+    return dtype == AUG_BF16 ? f((__bf16)0) : dtype == AUG_F16 ? f((_Float16)0) : f(0.f);
+}
+
+template <class T> __device__ inline const T* row_in(const aug_rows& m, int64_t r) { return static_cast<const T*>(m.data) + r * m.ld; }
+template <class T> __device__ inline T* row_out(const aug_rows& m, int64_t r) { return static_cast<T*>(m.data) + r * m.ld; }
+
+constexpr float kLog2e = 1.44269504088896341f;
+
+// exp(x) by the hardware's power of two, whose argument's rounding is 2^-24 |x log2 e| of the result.
+__device__ inline float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+__device__ inline float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + exp_fast(-x)); }      // 0 and 1 at the infinities
+// ln(1 + exp(x)) = max(x, 0) + ln(1 + e), e = exp(-|x|).  With w = 1 + e rounded, ln(w) e / (w - 1) has the relative accuracy
+// of ln: the rounding of w is in both (for e below half a step of 1, w is 1 and the value e).
+__device__ inline float softplus(float x) {
+    const float e = exp_fast(-fabsf(x)), w = 1.f + e, d = w - 1.f;
+    const float l = d == 0.f ? e : __builtin_amdgcn_logf(w) * 0.693147180559945309f * (e * __builtin_amdgcn_rcpf(d));
+    return fmaxf(x, 0.f) + l;      // (a NaN is in l, whatever fmaxf drops)
+}
+
+__device__ inline float wave_sum(float v) {
+    for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
+    return v;
+}
+// The larger of two magnitudes' bits: a NaN's are larger than any number's.
+__device__ inline unsigned wave_max(unsigned v) {
+    for (int m = 32; m; m >>= 1) {
+        const unsigned o = __shfl_xor(v, m);
+        v = v > o ? v : o;
+    }
+    return v;
+}
+
+}  // namespace aug

@@ -1,0 +1,80 @@
+// The operators on feature rows: what the C ABI hands to their launchers (which check nothing).
+#pragma once
+
+#include "aug_internal.h"
+
+namespace aug {
+
+// The sequences of a call, cut into blocks of 1 << lg rows.
+struct RowBlocks {
+    int n_seq = 0, lg = 0, n_items = 0;
+    const int64_t* begin = nullptr;      // device [n_seq+1]
+    const int64_t* end = nullptr;        // device [n_seq+1]
+    const int* first = nullptr;          // device [n_seq+1]: blocks of the sequences before i
+    const int2* items = nullptr;         // device [n_items]: (sequence, block of it)
+};
+
+// out[c] = sum over p < n_partial of partial[p * stride + c], c < width; in that order, so that the result has one value.
+hipError_t launch_sum_partials(hipStream_t s, const float* partial, int n_partial, int64_t stride, int64_t width, float* out);
+
+struct NormArgs {
+    int64_t n_rows;
+    aug_norm_cfg cfg;
+    aug_rows x, residual, sum, y, q;     // data null: not there
+    const float* weight;
+    float* scale;
+    float* rstd;
+};
+hipError_t launch_norm(hipStream_t s, const NormArgs& a, int n_cu);
+
+struct NormBackArgs {
+    int64_t n_rows;
+    int dtype, dim;
+    aug_rows sum, dy, dsum, dx;
+    const float* weight;
+    const float* rstd;
+    float* dweight;
+    float* partial;                      // [norm_partials][dim], used with dweight
+};
+int norm_partials(int64_t n_rows, int dim, int n_cu);
+hipError_t launch_norm_backward(hipStream_t s, const NormBackArgs& a, int n_cu);
+
+struct ShortConvArgs {
+    RowBlocks rows;
+    aug_short_conv_cfg cfg;
+    aug_rows x, y;
+    const float* weight;
+    const float* bias;
+    const void* state_in;
+    void* state_out;
+    // gradients
+    aug_rows dy, dx;
+    float* dweight;
+    float* dbias;
+    float* partial;                      // [short_conv_partials][dim * (taps + 1)]: by the weight, then by the bias
+};
+int short_conv_lg_block(const aug_short_conv_cfg& cfg, bool backward);       // rows of a block, as a power of two
+int short_conv_partials(const aug_short_conv_cfg& cfg, int n_items, int n_cu);
+hipError_t launch_short_conv(hipStream_t s, const ShortConvArgs& a);
+hipError_t launch_short_conv_backward(hipStream_t s, const ShortConvArgs& a, int n_cu);
+hipError_t launch_short_conv_step(hipStream_t s, int n_seq, const ShortConvArgs& a);
+
+struct ScanArgs {
+    RowBlocks rows;
+    aug_scan_cfg cfg;
+    aug_scan_in in;
+    const float* state_in;
+    float* state_out;
+    aug_rows y;
+    // gradients
+    aug_rows dy;
+    aug_scan_grad grad;
+    void* ws;
+};
+int scan_lg_block(const aug_scan_cfg& cfg, int n_seq, const int64_t* begin, const int64_t* end, int n_cu, bool backward);
+size_t scan_workspace(const aug_scan_cfg& cfg, int n_items, int64_t n_rows, int n_cu, bool backward);     // bytes
+hipError_t launch_scan(hipStream_t s, const ScanArgs& a, int n_cu);
+hipError_t launch_scan_backward(hipStream_t s, const ScanArgs& a, int64_t n_rows, int n_cu);
+hipError_t launch_scan_step(hipStream_t s, int n_seq, const ScanArgs& a);
+
+}  // namespace aug
