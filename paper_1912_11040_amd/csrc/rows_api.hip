@@ -477,8 +477,10 @@ int aug_scan_batch(aug_ctx* ctx, int n_seq, const int64_t* row_offsets, const in
         AUG_TRY(sp.check(ctx));
         if (n_seq == 0 || (seq.total == 0 && !state_out)) return AUG_OK;
         AUG_TRY(seq.plan(aug::scan_lg_block(*cfg, n_seq, row_offsets, row_lengths, ctx->n_cu, false)));
-        AUG_TRY(grow(ctx, ctx->seq_ws, aug::scan_workspace(*cfg, seq.blocks.n_items, seq.n_rows, ctx->n_cu, false), "scan workspace"));
-        a.ws = ctx->seq_ws.ptr;
+        if (seq.blocks.lg < 30) {            // sequences in one piece need none
+            AUG_TRY(grow(ctx, ctx->seq_ws, aug::scan_workspace(*cfg, seq.blocks.n_items, seq.n_rows, ctx->n_cu, false), "scan workspace"));
+            a.ws = ctx->seq_ws.ptr;
+        }
         AUG_TRY(seq.launch());
         a.rows = seq.blocks;
         AUG_TRY(mark(ctx, -1));

@@ -13,6 +13,44 @@ template <class F> hipError_t with_type(int dtype, F f) {
 template <class T> __device__ inline const T* row_in(const aug_rows& m, int64_t r) { return static_cast<const T*>(m.data) + r * m.ld; }
 template <class T> __device__ inline T* row_out(const aug_rows& m, int64_t r) { return static_cast<T*>(m.data) + r * m.ld; }
 
+// N elements next to each other, aligned as one element is: wide accesses, which the hardware allows at any such address.
+template <class T, int N> struct Pack {
+    T v[N];
+};
+// Elements 0 .. valid - 1 of the N at p (zeros behind them; valid may be negative); nothing else is touched.
+template <class T, int N> __device__ inline Pack<T, N> load_pack(const T* p, int valid) {
+    Pack<T, N> r;
+    if (valid >= N) {
+        __builtin_memcpy(r.v, p, sizeof r);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) r.v[i] = i < valid ? p[i] : (T)0;
+    }
+    return r;
+}
+template <class T, int N> __device__ inline void store_pack(T* p, const Pack<T, N>& r, int valid) {
+    if (valid >= N) {
+        __builtin_memcpy(p, r.v, sizeof r);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (i < valid) p[i] = r.v[i];
+}
+
+// The sum over LN (a power of two up to 16) neighbouring lanes, in all of them: quads by permutation, then mirrored halves, whose
+// lanes hold equal sums already.
+template <int CTRL> __device__ inline float dpp_add(float v) {
+    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+template <int LN> __device__ inline float lanes_sum(float v) {
+    if constexpr (LN >= 2) v = dpp_add<0xB1>(v);
+    if constexpr (LN >= 4) v = dpp_add<0x4E>(v);
+    if constexpr (LN >= 8) v = dpp_add<0x141>(v);
+    if constexpr (LN >= 16) v = dpp_add<0x140>(v);
+    return v;
+}
+
 constexpr float kLog2e = 1.44269504088896341f;
 
 // exp(x) by the hardware's power of two, whose argument's rounding is 2^-24 |x log2 e| of the result.

@@ -71,7 +71,7 @@ struct ScanArgs {
     aug_scan_grad grad;
     void* ws;
 };
-int scan_lg_block(const aug_scan_cfg& cfg, int n_seq, const int64_t* begin, const int64_t* end, int n_cu, bool backward);
+int scan_lg_block(const aug_scan_cfg& cfg, int n_seq, const int64_t* begin, const int64_t* lengths, int n_cu, bool backward);
 size_t scan_workspace(const aug_scan_cfg& cfg, int n_items, int64_t n_rows, int n_cu, bool backward);     // bytes
 hipError_t launch_scan(hipStream_t s, const ScanArgs& a, int n_cu);
 hipError_t launch_scan_backward(hipStream_t s, const ScanArgs& a, int64_t n_rows, int n_cu);
