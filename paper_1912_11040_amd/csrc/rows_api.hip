@@ -564,7 +564,7 @@ int aug_scan_step(aug_ctx* ctx, int n_seq, const aug_scan_cfg* cfg, const aug_sc
         sp.add("y_out", a.y.data, a.y.ld * e, cfg->dim * e, n_seq, 1, bits);
         AUG_TRY(sp.check(ctx));
         AUG_TRY(mark(ctx, -1));
-        AUG_HIP(aug::launch_scan_step(ctx->stream, n_seq, a), "scan kernel");
+        AUG_HIP(aug::launch_scan_step(ctx->stream, n_seq, a, ctx->n_cu), "scan kernel");
         return mark(ctx, AUG_STAGE_SCAN);
     });
 }

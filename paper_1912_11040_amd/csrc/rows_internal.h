@@ -75,6 +75,6 @@ int scan_lg_block(const aug_scan_cfg& cfg, int n_seq, const int64_t* begin, cons
 size_t scan_workspace(const aug_scan_cfg& cfg, int n_items, int64_t n_rows, int n_cu, bool backward);     // bytes
 hipError_t launch_scan(hipStream_t s, const ScanArgs& a, int n_cu);
 hipError_t launch_scan_backward(hipStream_t s, const ScanArgs& a, int64_t n_rows, int n_cu);
-hipError_t launch_scan_step(hipStream_t s, int n_seq, const ScanArgs& a);
+hipError_t launch_scan_step(hipStream_t s, int n_seq, const ScanArgs& a, int n_cu);
 
 }  // namespace aug

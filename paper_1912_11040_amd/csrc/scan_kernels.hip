@@ -191,30 +191,42 @@ __global__ __launch_bounds__(64) void scan_join_kernel(ScanArgs a, float* first_
 }
 
 // ---- rows of streams ----
-// A thread per (stream, channel).
-template <class T>
-__global__ __launch_bounds__(kChannels) void scan_step_kernel(ScanArgs a) {
-    extern __shared__ float h[];
-    const int lane = threadIdx.x, d = blockIdx.y * kChannels + lane, n_state = a.cfg.n_state;
-    const int64_t r = blockIdx.x;
-    if (d >= a.cfg.dim) return;
-    const int64_t at = (r * a.cfg.dim + d) * n_state;
-    const int g = d / (a.cfg.dim / a.cfg.n_group);
+// The same lanes per channel; a group takes 256 / LN channels, whose rates stay in registers, through `streams` rows.
+template <class T, int LN, int K>
+__global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, int n_seq, int streams) {
+    using G = Tile<LN, K>;
+    const int tid = threadIdx.x, dim = a.cfg.dim, n_state = a.cfg.n_state, per_group = dim / a.cfg.n_group;
+    const int tiles = (per_group + G::CW - 1) / G::CW, group = blockIdx.x / tiles;
+    const int in_group = (blockIdx.x % tiles) * G::CW + tid / LN, nq = (tid % LN) * K, states = n_state - nq;
+    if (in_group >= per_group) return;                   // (all lanes of a channel together)
+    const int d = group * per_group + in_group;
+    const Pack<float, K> rates = load_pack<float, K>(a.in.a + (int64_t)d * n_state + nq, states);
+    float rate[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) rate[k] = rate2(rates.v[k]);
     const float bias = a.in.delta_bias ? a.in.delta_bias[d] : 0.f, skip = a.in.skip ? a.in.skip[d] : 0.f;
-    const float u = (float)row_in<T>(a.in.u, r)[d], step = step_of(a.cfg, (float)row_in<T>(a.in.delta, r)[d] + bias);
-    const T* b = row_in<T>(a.in.b, r) + (int64_t)g * n_state;
-    const T* c = row_in<T>(a.in.c, r) + (int64_t)g * n_state;
-    float p = skip * u;
-    for (int n = 0; n < n_state; ++n) {
-        const float v = fmaf(exp_fast(step * a.in.a[(int64_t)d * n_state + n]), a.state_in[at + n], step * u * (float)b[n]);
-        a.state_out[at + n] = v;
-        p = fmaf((float)c[n], v, p);
+    const int from = blockIdx.y * streams, to = min(from + streams, n_seq);
+    const int64_t col = (int64_t)group * n_state + nq;
+#pragma unroll 4
+    for (int r = from; r < to; ++r) {
+        const int64_t at = ((int64_t)r * dim + d) * n_state + nq;
+        Pack<float, K> h = load_pack<float, K>(a.state_in + at, states);
+        const Pack<T, K> b = load_pack<T, K>(row_in<T>(a.in.b, r) + col, states), c = load_pack<T, K>(row_in<T>(a.in.c, r) + col, states);
+        const float u = (float)row_in<T>(a.in.u, r)[d], step = step_of(a.cfg, (float)row_in<T>(a.in.delta, r)[d] + bias), su = step * u;
+        float p = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            h.v[k] = fmaf(__builtin_amdgcn_exp2f(step * rate[k]), h.v[k], su * (float)b.v[k]);
+            if (k < states) p = fmaf((float)c.v[k], h.v[k], p);
+        }
+        p = fmaf(skip, u, lanes_sum<LN>(p));
+        store_pack<float, K>(a.state_out + at, h, states);
+        if (a.in.z.data) {
+            const float z = (float)row_in<T>(a.in.z, r)[d];
+            p *= z * sigmoid(z);
+        }
+        if (tid % LN == 0) row_out<T>(a.y, r)[d] = (T)p;
     }
-    if (a.in.z.data) {
-        const float z = (float)row_in<T>(a.in.z, r)[d];
-        p *= z * sigmoid(z);
-    }
-    row_out<T>(a.y, r)[d] = (T)p;
 }
 
 // ---- gradients ----
@@ -393,10 +405,16 @@ hipError_t launch_scan(hipStream_t s, const ScanArgs& a, int) {
     });
 }
 
-hipError_t launch_scan_step(hipStream_t s, int n_seq, const ScanArgs& a) {
+hipError_t launch_scan_step(hipStream_t s, int n_seq, const ScanArgs& a, int n_cu) {
+    // as many streams to a group as leave eight groups to a compute unit
+    const int64_t tiles = scan_tiles(a.cfg), each = n_seq * tiles / (8 * (int64_t)n_cu);
+    const int streams = each < 1 ? 1 : each > 16 ? 16 : (int)each;
     return with_type(a.cfg.dtype, [&](auto t) {
-        scan_step_kernel<decltype(t)><<<dim3((unsigned)n_seq, (unsigned)((a.cfg.dim + kChannels - 1) / kChannels)), dim3(kChannels), 0, s>>>(a);
-        return hipGetLastError();
+        return with_lanes(a.cfg.n_state, [&](auto ln, auto k) {
+            scan_step_kernel<decltype(t), ln.value, k.value>
+                <<<dim3((unsigned)tiles, (unsigned)((n_seq + streams - 1) / streams)), dim3(256), 0, s>>>(a, n_seq, streams);
+            return hipGetLastError();
+        });
     });
 }
 
