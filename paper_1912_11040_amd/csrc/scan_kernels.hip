@@ -7,13 +7,11 @@
 namespace aug {
 namespace {
 
-constexpr int kChannels = 64;            // (of the gradients' and the streams' groups)
-
 __device__ inline float step_of(const aug_scan_cfg& cfg, float v) { return cfg.softplus ? softplus(v) : v; }
-// The rate for powers of two.  (The lowest finite numbers stay finite: a step of zero keeps their state.)
+// The rate for powers of two, finite also for the lowest numbers: a step of zero keeps the state.
 __device__ inline float rate2(float a) {
     const float r = a * kLog2e;
-    return r < -3.4e38f && a > -INFINITY ? -3.4e38f : r;
+    return r < -3.4e38f ? -3.4e38f : r;
 }
 
 // ---- rows of sequences ----
@@ -207,7 +205,6 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, int n_seq, i
     const float bias = a.in.delta_bias ? a.in.delta_bias[d] : 0.f, skip = a.in.skip ? a.in.skip[d] : 0.f;
     const int from = blockIdx.y * streams, to = min(from + streams, n_seq);
     const int64_t col = (int64_t)group * n_state + nq;
-#pragma unroll 4
     for (int r = from; r < to; ++r) {
         const int64_t at = ((int64_t)r * dim + d) * n_state + nq;
         Pack<float, K> h = load_pack<float, K>(a.state_in + at, states);
@@ -230,115 +227,363 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, int n_seq, i
 }
 
 // ---- gradients ----
-// Workspace of the gradients: states behind every row [rows][dim][n_state], sums of a tile of channels for db and dc
-// [tiles][rows][2 n_state], for da, dskip and ddelta_bias [n_seq][dim][n_state + 2].
-struct BackWs {
-    float *h, *bc, *par;
+//
+// Sequences are cut into blocks of 1 << lg rows.  A first pass over each block forms, in one walk over its decays,
+//   F, the end state from zero,  S, the sum of the steps,  R = sum_t (e_first .. e_t) c_t dp_t,
+// the block's share of e_first g_first, which is what it hands to the rows before it.  scan_back_join_kernel then makes of F the state
+// before each block and of R what comes in from behind.  With both the blocks are independent of one another: the main pass
+// walks a block forward for its states and back for its gradients, in stretches of SUB rows whose states and decays stay in registers.
+template <int LN, int K> struct BackTile {
+    static constexpr int CW = 256 / LN, NP = LN * K, LG = NP <= 64 ? 5 : 4, RT = 1 << LG, EPT = RT * CW / 256, SUB = K <= 4 ? 16 : 8;
+    static constexpr int BC = (RT * NP + 255) / 256;
 };
-__host__ __device__ inline int tiles_of(const aug_scan_cfg& cfg) {
-    return cfg.n_group * ((cfg.dim / cfg.n_group + kChannels - 1) / kChannels);
-}
-__host__ __device__ inline BackWs back_ws(const aug_scan_cfg& cfg, void* ws, int64_t n_rows) {
+
+// Workspace: first states and what comes in from behind [items][dim][n_state], steps' sums [items][dim]; sums over a tile of channels for
+// db and dc [tiles][n_rows][2 n_state]; sums over a run of blocks for da, dskip and ddelta_bias [runs][dim][n_state + 2].
+struct BackWs {
+    float *first, *behind, *steps, *bc, *par;
+};
+struct BackPlan {
+    int tiles, runs;                     // channel tiles (all groups'); runs of blocks, a group's work in the main pass
+};
+__host__ __device__ inline BackWs back_ws(const aug_scan_cfg& cfg, void* ws, int n_items, int64_t n_rows, int tiles) {
     BackWs w;
-    w.h = static_cast<float*>(ws);
-    w.bc = w.h + n_rows * cfg.dim * cfg.n_state;
-    w.par = w.bc + (int64_t)tiles_of(cfg) * n_rows * 2 * cfg.n_state;
+    const int64_t states = (int64_t)n_items * cfg.dim * cfg.n_state;
+    w.first = static_cast<float*>(ws);
+    w.behind = w.first + states;
+    w.steps = w.behind + states;
+    w.bc = w.steps + (int64_t)n_items * cfg.dim;
+    w.par = w.bc + (int64_t)tiles * n_rows * 2 * cfg.n_state;
     return w;
 }
 
-// A wavefront per (sequence, tile of up to 64 channels of one group).
-template <class T>
-__global__ __launch_bounds__(kChannels) void scan_backward_kernel(ScanArgs a, int64_t n_rows) {
-    extern __shared__ float g[];                        // decay times gradient of the row behind, then da: [2][n_state][64]
-    const int lane = threadIdx.x, n_state = a.cfg.n_state, dim = a.cfg.dim, per_group = dim / a.cfg.n_group;
-    const int tiles = (per_group + kChannels - 1) / kChannels, group = blockIdx.y / tiles;
-    const int in_group = (blockIdx.y % tiles) * kChannels + lane;
-    const bool live = in_group < per_group;
-    const int d = group * per_group + (live ? in_group : 0);
-    const int64_t seq = blockIdx.x, begin = a.rows.begin[seq], end = a.rows.end[seq];
-    const BackWs ws = back_ws(a.cfg, a.ws, n_rows);
-    const float* rate = a.in.a + (int64_t)d * n_state;
-    float* const da = g + n_state * kChannels;
-    const float bias = a.in.delta_bias ? a.in.delta_bias[d] : 0.f, skip = a.in.skip ? a.in.skip[d] : 0.f;
-    float* const par = ws.par + (seq * dim + d) * (n_state + 2);
-    for (int n = 0; n < n_state; ++n) g[n * kChannels + lane] = da[n * kChannels + lane] = 0.f;
-    if (live)
-        for (int64_t r = begin; r < end; ++r) {
-            const float u = (float)row_in<T>(a.in.u, r)[d], step = step_of(a.cfg, (float)row_in<T>(a.in.delta, r)[d] + bias);
-            const T* b = row_in<T>(a.in.b, r) + (int64_t)group * n_state;
-            float* const h = ws.h + (r * dim + d) * n_state;
-            const float* const before = r > begin ? h - (int64_t)dim * n_state : a.state_in ? a.state_in + (seq * dim + d) * n_state : nullptr;
-            for (int n = 0; n < n_state; ++n) h[n] = fmaf(exp_fast(step * rate[n]), before ? before[n] : 0.f, step * u * (float)b[n]);
-        }
-    float dskip = 0.f, dbias = 0.f;
-    for (int64_t r = end - 1; r >= begin; --r) {
-        const float u = (float)row_in<T>(a.in.u, r)[d], raw = (float)row_in<T>(a.in.delta, r)[d] + bias, step = step_of(a.cfg, raw);
-        const T* b = row_in<T>(a.in.b, r) + (int64_t)group * n_state;
-        const T* c = row_in<T>(a.in.c, r) + (int64_t)group * n_state;
-        const float dy = (float)row_in<T>(a.dy, r)[d], z = a.in.z.data ? (float)row_in<T>(a.in.z, r)[d] : 0.f;
-        const float sz = sigmoid(z), dp = live ? (a.in.z.data ? dy * z * sz : dy) : 0.f;
-        float* const h = ws.h + (r * dim + d) * n_state;
-        const float* const before = r > begin ? h - (int64_t)dim * n_state : a.state_in ? a.state_in + (seq * dim + d) * n_state : nullptr;
-        float p = skip * u, gb = 0.f, dstep = 0.f;
-        float* const bc = ws.bc + ((int64_t)blockIdx.y * n_rows + r) * 2 * n_state;
-        for (int n = 0; n < n_state; ++n) {
-            const float e = exp_fast(step * rate[n]), gr = fmaf((float)c[n], dp, g[n * kChannels + lane]), eg = e * gr;
-            const float eh = eg * (before ? before[n] : 0.f), hn = live ? h[n] : 0.f;
-            g[n * kChannels + lane] = eg;
-            p = fmaf((float)c[n], hn, p);
-            gb = fmaf(gr, (float)b[n], gb);
-            dstep = fmaf(eh, rate[n], dstep);
-            da[n * kChannels + lane] += eh * step;
-            const float db = wave_sum(live ? gr * step * u : 0.f), dc = wave_sum(live ? dp * hn : 0.f);
-            if (lane == 0) bc[n] = db, bc[n_state + n] = dc;
-        }
-        if (!live) continue;
-        dskip = fmaf(dp, u, dskip);
-        dstep = fmaf(u, gb, dstep);
-        const float dd = a.cfg.softplus ? dstep * sigmoid(raw) : dstep;
-        dbias += dd;
-        if (a.grad.du.data) row_out<T>(a.grad.du, r)[d] = (T)(step * gb + skip * dp);
-        if (a.grad.ddelta.data) row_out<T>(a.grad.ddelta, r)[d] = (T)dd;
-        if (a.grad.dz.data) row_out<T>(a.grad.dz, r)[d] = (T)(dy * p * sz * (1.f + z * (1.f - sz)));
+// Halves an array of N values by bit 5 or 4 of the lane: lanes without it keep the first half's sums over the two, lanes with
+// it the second's.
+template <int BIT, int N, int V> __device__ inline void halve(float (&v)[V]) {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+        const unsigned x = __float_as_uint(v[i]), y = __float_as_uint(v[i + N / 2]);
+        const auto r = BIT == 5 ? __builtin_amdgcn_permlane32_swap(x, y, false, false) : __builtin_amdgcn_permlane16_swap(x, y, false, false);
+        v[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
     }
-    if (!live) return;
-    for (int n = 0; n < n_state; ++n) par[n] = da[n * kChannels + lane];
-    par[n_state] = dskip;
-    par[n_state + 1] = dbias;
 }
 
-// db and dc: sums over the tiles of a group.  A group per sequence, so that rows of none are left alone.
+template <class T, int LN, int K>
+__global__ __launch_bounds__(256) void scan_back_sums_kernel(ScanArgs a, BackWs ws) {
+    using G = BackTile<LN, K>;
+    __shared__ float2 su[G::RT][G::CW];
+    __shared__ float sdp[G::RT][G::CW];
+    __shared__ float sb[G::RT][G::NP], sc[G::RT][G::NP];
+    const int tid = threadIdx.x, dim = a.cfg.dim, n_state = a.cfg.n_state, per_group = dim / a.cfg.n_group;
+    const int tiles = (per_group + G::CW - 1) / G::CW, group = blockIdx.x / tiles, in_group = (blockIdx.x % tiles) * G::CW;
+    const int d0 = group * per_group + in_group, width = min(G::CW, per_group - in_group);
+    const int2 item = a.rows.items[blockIdx.y];
+    const int64_t begin = a.rows.begin[item.x] + ((int64_t)item.y << G::LG), end = a.rows.end[item.x];
+    const int here = (int)min(end - begin, (int64_t)G::RT);
+    if (here <= 0) return;
+    const int lt = tid / (G::CW / G::EPT), lc = tid % (G::CW / G::EPT) * G::EPT, valid = lt < here ? width - lc : 0;
+    const int64_t r = begin + lt;
+    const auto u = load_pack<T, G::EPT>(row_in<T>(a.in.u, r) + d0 + lc, valid);
+    const auto delta = load_pack<T, G::EPT>(row_in<T>(a.in.delta, r) + d0 + lc, valid);
+    const auto dy = load_pack<T, G::EPT>(row_in<T>(a.dy, r) + d0 + lc, valid);
+    Pack<T, G::EPT> z;
+    if (a.in.z.data) z = load_pack<T, G::EPT>(row_in<T>(a.in.z, r) + d0 + lc, valid);
+#pragma unroll
+    for (int j = 0; j < G::BC; ++j) {
+        const int e = tid + 256 * j, t = e / G::NP, n = e % G::NP;
+        if (t >= G::RT) break;
+        const bool there = t < here && n < n_state;
+        const int64_t col = (int64_t)group * n_state + n;
+        sb[t][n] = there ? (float)row_in<T>(a.in.b, begin + t)[col] : 0.f;
+        sc[t][n] = there ? (float)row_in<T>(a.in.c, begin + t)[col] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < G::EPT; ++i) {
+        const float step = i < valid ? step_of(a.cfg, (float)delta.v[i] + (a.in.delta_bias ? a.in.delta_bias[d0 + lc + i] : 0.f)) : 0.f;
+        su[lt][lc + i] = make_float2(step, step * (float)u.v[i]);
+        float dp = (float)dy.v[i];
+        if (a.in.z.data) dp *= (float)z.v[i] * sigmoid((float)z.v[i]);
+        sdp[lt][lc + i] = dp;
+    }
+    __syncthreads();
+    const int ch = tid / LN, nq = (tid % LN) * K;
+    if (ch >= width) return;
+    const int64_t at = ((int64_t)blockIdx.y * dim + d0 + ch) * n_state + nq;
+    float f[K] = {}, q[K], back[K] = {}, rate[K], sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        rate[k] = nq + k < n_state ? rate2(a.in.a[(int64_t)(d0 + ch) * n_state + nq + k]) : 0.f;
+        q[k] = 1.f;
+    }
+#pragma unroll 4
+    for (int t = 0; t < here; ++t) {
+        const float2 s = su[t][ch];
+        const float dp = sdp[t][ch];
+        sum += s.x;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const float e = __builtin_amdgcn_exp2f(s.x * rate[k]);
+            f[k] = fmaf(e, f[k], s.y * sb[t][nq + k]);
+            q[k] *= e;
+            back[k] = fmaf(q[k], sc[t][nq + k] * dp, back[k]);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (nq + k < n_state) ws.first[at + k] = f[k], ws.behind[at + k] = back[k];
+    if (tid % LN == 0) ws.steps[(int64_t)blockIdx.y * dim + d0 + ch] = sum;
+}
+
+// A thread per (sequence, state): forward through the blocks for their first states, back for what comes in from behind.
+__global__ __launch_bounds__(64) void scan_back_join_kernel(ScanArgs a, BackWs ws) {
+    const int64_t width = (int64_t)a.cfg.dim * a.cfg.n_state, i = (int64_t)blockIdx.x * 64 + threadIdx.x;
+    const int seq = blockIdx.y, from = a.rows.first[seq], to = a.rows.first[seq + 1];
+    if (i >= width || a.rows.end[seq] == a.rows.begin[seq]) return;
+    const int64_t d = i / a.cfg.n_state;
+    const float rate = rate2(a.in.a[i]);
+    constexpr int kAhead = 8;
+    float h = a.state_in ? a.state_in[seq * width + i] : 0.f;
+    for (int at = from; at < to; at += kAhead) {
+        float f[kAhead], s[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            f[j] = at + j < to ? ws.first[(at + j) * width + i] : 0.f;
+            s[j] = at + j < to ? ws.steps[(int64_t)(at + j) * a.cfg.dim + d] : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            if (at + j < to) ws.first[(at + j) * width + i] = h;
+            h = h == 0.f ? f[j] : fmaf(__builtin_amdgcn_exp2f(s[j] * rate), h, f[j]);
+        }
+    }
+    float g = 0.f;
+    for (int at = to - 1; at >= from; at -= kAhead) {
+        float f[kAhead], s[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            f[j] = at - j >= from ? ws.behind[(at - j) * width + i] : 0.f;
+            s[j] = at - j >= from ? ws.steps[(int64_t)(at - j) * a.cfg.dim + d] : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            if (at - j >= from) ws.behind[(at - j) * width + i] = g;
+            g = g == 0.f ? f[j] : fmaf(__builtin_amdgcn_exp2f(s[j] * rate), g, f[j]);
+        }
+    }
+}
+
+template <class T, int LN, int K>
+__global__ __launch_bounds__(256) void scan_back_kernel(ScanArgs a, BackWs ws, BackPlan plan, int64_t n_rows, bool joined) {
+    using G = BackTile<LN, K>;
+    constexpr int NS = G::RT / G::SUB, V = 2 * K;
+    __shared__ float2 su[G::RT][G::CW];                  // (step, step u); behind a row's walk (sum g b, sum of e g h a)
+    __shared__ float sdp[G::RT][G::CW];                  // dp; behind a row's walk sum c h
+    __shared__ float sb[G::RT][G::NP], sc[G::RT][G::NP];
+    __shared__ float sbc[4][G::RT][2 * G::NP];           // each wavefront's sums over its channels for db and dc
+    const int tid = threadIdx.x, dim = a.cfg.dim, n_state = a.cfg.n_state, per_group = dim / a.cfg.n_group;
+    const int tile = blockIdx.x % plan.tiles, run = blockIdx.x / plan.tiles;
+    const int tiles = plan.tiles / a.cfg.n_group, group = tile / tiles, in_group = (tile % tiles) * G::CW;
+    const int d0 = group * per_group + in_group, width = min(G::CW, per_group - in_group);
+    const int first_item = (int)((int64_t)a.rows.n_items * run / plan.runs), end_item = (int)((int64_t)a.rows.n_items * (run + 1) / plan.runs);
+
+    const int ch = tid / LN, nq = (tid % LN) * K, wave = tid / 64;
+    const bool walks = ch < width;
+    float rate[K], da[K] = {};
+#pragma unroll
+    for (int k = 0; k < K; ++k) rate[k] = walks && nq + k < n_state ? rate2(a.in.a[(int64_t)(d0 + ch) * n_state + nq + k]) : 0.f;
+    const int lt = tid / (G::CW / G::EPT), lc = tid % (G::CW / G::EPT) * G::EPT;
+    float bias[G::EPT], skip[G::EPT], dskip[G::EPT] = {}, dbias[G::EPT] = {};
+#pragma unroll
+    for (int i = 0; i < G::EPT; ++i) {
+        bias[i] = a.in.delta_bias && lc + i < width ? a.in.delta_bias[d0 + lc + i] : 0.f;
+        skip[i] = a.in.skip && lc + i < width ? a.in.skip[d0 + lc + i] : 0.f;
+    }
+    const bool gate = a.in.z.data;
+
+    for (int it = first_item; it < end_item; ++it) {
+        const int2 item = a.rows.items[it];
+        const int64_t from = a.rows.begin[item.x], begin = from + ((int64_t)item.y << G::LG), end = a.rows.end[item.x];
+        const int here = (int)min(end - begin, (int64_t)G::RT);
+        if (here <= 0) continue;                         // (an empty sequence's block)
+        const int valid = lt < here ? width - lc : 0;
+        const int64_t r = begin + lt;
+        const auto u = load_pack<T, G::EPT>(row_in<T>(a.in.u, r) + d0 + lc, valid);
+        const auto delta = load_pack<T, G::EPT>(row_in<T>(a.in.delta, r) + d0 + lc, valid);
+        const auto dy = load_pack<T, G::EPT>(row_in<T>(a.dy, r) + d0 + lc, valid);
+        Pack<T, G::EPT> z;
+        if (gate) z = load_pack<T, G::EPT>(row_in<T>(a.in.z, r) + d0 + lc, valid);
+#pragma unroll
+        for (int j = 0; j < G::BC; ++j) {
+            const int e = tid + 256 * j, t = e / G::NP, n = e % G::NP;
+            if (t >= G::RT) break;
+            const bool there = t < here && n < n_state;
+            const int64_t col = (int64_t)group * n_state + n;
+            sb[t][n] = there ? (float)row_in<T>(a.in.b, begin + t)[col] : 0.f;
+            sc[t][n] = there ? (float)row_in<T>(a.in.c, begin + t)[col] : 0.f;
+        }
+        // the state before the block, and what comes in from behind it: e g of the row behind
+        float st[NS][K], carried[K];
+        {
+            const int64_t at = ((int64_t)it * dim + d0 + ch) * n_state + nq, in = ((int64_t)item.x * dim + d0 + ch) * n_state + nq;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const bool there = walks && nq + k < n_state;
+                st[0][k] = !there ? 0.f : joined ? ws.first[at + k] : a.state_in ? a.state_in[in + k] : 0.f;
+                carried[k] = there && joined ? ws.behind[at + k] : 0.f;
+            }
+        }
+        float step[G::EPT];
+#pragma unroll
+        for (int i = 0; i < G::EPT; ++i) {
+            step[i] = i < valid ? step_of(a.cfg, (float)delta.v[i] + bias[i]) : 0.f;
+            su[lt][lc + i] = make_float2(step[i], step[i] * (float)u.v[i]);
+            float dp = (float)dy.v[i];
+            if (gate) dp *= (float)z.v[i] * sigmoid((float)z.v[i]);
+            sdp[lt][lc + i] = dp;
+        }
+        __syncthreads();
+        // states before the later stretches
+#pragma unroll
+        for (int s = 0; s + 1 < NS; ++s) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) st[s + 1][k] = st[s][k];
+            if ((s + 1) * G::SUB < here) {
+#pragma unroll 4
+                for (int t = s * G::SUB; t < (s + 1) * G::SUB; ++t) {
+                    const float2 x = su[t][ch];
+#pragma unroll
+                    for (int k = 0; k < K; ++k) st[s + 1][k] = fmaf(__builtin_amdgcn_exp2f(x.x * rate[k]), st[s + 1][k], x.y * sb[t][nq + k]);
+                }
+            }
+        }
+#pragma unroll
+        for (int s = NS - 1; s >= 0; --s) {
+            if (s * G::SUB >= here) continue;            // (rows behind the sequence's end inside a stretch have steps and dp of zero)
+            float h[G::SUB + 1][K], e[G::SUB][K];
+#pragma unroll
+            for (int k = 0; k < K; ++k) h[0][k] = st[s][k];
+#pragma unroll
+            for (int j = 0; j < G::SUB; ++j) {
+                const int t = s * G::SUB + j;
+                const float2 x = su[t][ch];
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    e[j][k] = __builtin_amdgcn_exp2f(x.x * rate[k]);
+                    h[j + 1][k] = fmaf(e[j][k], h[j][k], x.y * sb[t][nq + k]);
+                }
+            }
+            float keep_gb = 0.f, keep_eh = 0.f, keep_p = 0.f;
+#pragma unroll
+            for (int j = G::SUB - 1; j >= 0; --j) {
+                const int t = s * G::SUB + j;
+                const float2 x = su[t][ch];
+                const float dp = sdp[t][ch];
+                float gb = 0.f, eha = 0.f, p = 0.f, v[V];
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    const float c = sc[t][nq + k], g = fmaf(c, dp, carried[k]);
+                    carried[k] = e[j][k] * g;
+                    const float eh = carried[k] * h[j][k];
+                    p = fmaf(c, h[j + 1][k], p);
+                    gb = fmaf(g, sb[t][nq + k], gb);
+                    eha = fmaf(eh, rate[k], eha);
+                    da[k] = fmaf(eh, x.x, da[k]);
+                    v[k] = g * x.y;
+                    v[K + k] = dp * h[j + 1][k];
+                }
+                gb = lanes_sum<LN>(gb);
+                eha = lanes_sum<LN>(eha);
+                p = lanes_sum<LN>(p);
+                // lane q of a channel keeps every LN-th row; the rows' steps are not read again
+                constexpr int kTurns = LN < G::SUB ? LN : G::SUB;
+                const bool mine = j % kTurns == tid % LN;
+                keep_gb = mine ? gb : keep_gb;
+                keep_eh = mine ? eha : keep_eh;
+                keep_p = mine ? p : keep_p;
+                if (j % kTurns == 0 && tid % LN < kTurns) {
+                    su[t + tid % LN][ch] = make_float2(keep_gb, keep_eh);
+                    sdp[t + tid % LN][ch] = keep_p;
+                }
+                // sums over the wavefront's channels (bits log2 LN .. 5 of the lane): a quarter of the values to each 16 lanes
+                halve<5, V>(v);
+                halve<4, V / 2>(v);
+#pragma unroll
+                for (int i = 0; i < V / 4; ++i) {
+                    if (LN <= 8) v[i] = dpp_add<0x128>(v[i]);              // lanes eight apart
+                    if (LN <= 4) v[i] = dpp_add<0x124>(v[i]);              // four apart (those eight apart are equal now)
+                }
+                const int lane = tid % 64, quarter = ((lane >> 5) * 2 + (lane >> 4 & 1)) * (V / 4);
+                if (LN <= 8 && V >= 8) {                 // half of them from lanes with bit 3
+                    const bool up = lane & 8;
+#pragma unroll
+                    for (int i = 0; i < V / 8; ++i) {
+                        const int val = quarter + i + (up ? V / 8 : 0);
+                        sbc[wave][t][val / K * G::NP + nq + val % K] = up ? v[i + V / 8] : v[i];
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < V / 4; ++i) {
+                        const int val = quarter + i;
+                        sbc[wave][t][val / K * G::NP + nq + val % K] = v[i];
+                    }
+                }
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < G::EPT; ++i) {
+            if (i >= valid) break;
+            const float2 x = su[lt][lc + i];
+            const float ui = (float)u.v[i], raw = (float)delta.v[i] + bias[i], dyi = (float)dy.v[i];
+            float dp = dyi;
+            if (gate) {
+                const float zi = (float)z.v[i], sg = sigmoid(zi);
+                dp = dyi * zi * sg;
+                if (a.grad.dz.data) row_out<T>(a.grad.dz, r)[d0 + lc + i] = (T)(dyi * fmaf(skip[i], ui, sdp[lt][lc + i]) * sg * (1.f + zi * (1.f - sg)));
+            }
+            const float dstep = fmaf(ui, x.x, x.y * 0.693147180559945309f);      // (the rates are those of powers of two)
+            const float dd = a.cfg.softplus ? dstep * sigmoid(raw) : dstep;
+            if (a.grad.du.data) row_out<T>(a.grad.du, r)[d0 + lc + i] = (T)fmaf(step[i], x.x, skip[i] * dp);
+            if (a.grad.ddelta.data) row_out<T>(a.grad.ddelta, r)[d0 + lc + i] = (T)dd;
+            dskip[i] = fmaf(dp, ui, dskip[i]);
+            dbias[i] += dd;
+        }
+        for (int e = tid; e < here * 2 * n_state; e += 256) {
+            const int t = e / (2 * n_state), n = e % (2 * n_state), at = n < n_state ? n : n - n_state + G::NP;
+            ws.bc[((int64_t)tile * n_rows + begin + t) * 2 * n_state + n] = (sbc[0][t][at] + sbc[1][t][at]) + (sbc[2][t][at] + sbc[3][t][at]);
+        }
+        __syncthreads();
+    }
+    if (!ws.par) return;
+    float* const par = ws.par + (int64_t)run * dim * (n_state + 2);
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (walks && nq + k < n_state) par[(int64_t)(d0 + ch) * n_state + nq + k] = da[k];
+    // over the rows of the tile, first to last
+#pragma unroll
+    for (int i = 0; i < G::EPT; ++i) su[lt][lc + i] = make_float2(dskip[i], dbias[i]);
+    __syncthreads();
+    if (tid >= width) return;
+    float ds = 0.f, db = 0.f;
+    for (int t = 0; t < G::RT; ++t) ds += su[t][tid].x, db += su[t][tid].y;
+    par[(int64_t)dim * n_state + d0 + tid] = ds;
+    par[(int64_t)dim * (n_state + 1) + d0 + tid] = db;
+}
+
+// db and dc: sums over the tiles of a group, a group of threads per block of rows.
 template <class T>
-__global__ __launch_bounds__(256) void scan_bc_kernel(ScanArgs a, int64_t n_rows) {
-    const int n_state = a.cfg.n_state, n_group = a.cfg.n_group, tiles = tiles_of(a.cfg) / n_group, width = 2 * n_state * n_group;
-    const int64_t seq = blockIdx.x, begin = a.rows.begin[seq], n = (a.rows.end[seq] - begin) * width;
-    const BackWs ws = back_ws(a.cfg, a.ws, n_rows);
-    for (int64_t i = threadIdx.x; i < n; i += 256) {
+__global__ __launch_bounds__(256) void scan_bc_kernel(ScanArgs a, BackWs ws, BackPlan plan, int64_t n_rows) {
+    const int n_state = a.cfg.n_state, n_group = a.cfg.n_group, tiles = plan.tiles / n_group, width = 2 * n_state * n_group;
+    const int2 item = a.rows.items[blockIdx.x];
+    const int64_t begin = a.rows.begin[item.x] + ((int64_t)item.y << a.rows.lg);
+    const int n = (int)min(a.rows.end[item.x] - begin, (int64_t)1 << a.rows.lg) * width;
+    for (int i = threadIdx.x; i < n; i += 256) {
         const int64_t r = begin + i / width;
-        const int group = (int)(i % width) / (2 * n_state), k = (int)(i % width) % (2 * n_state);
+        const int group = (i % width) / (2 * n_state), k = (i % width) % (2 * n_state);
         float acc = 0.f;
         for (int t = 0; t < tiles; ++t) acc += ws.bc[((int64_t)(group * tiles + t) * n_rows + r) * 2 * n_state + k];
         const aug_rows& out = k < n_state ? a.grad.db : a.grad.dc;
-        if (out.data) row_out<T>(out, r)[group * n_state + k % n_state] = (T)acc;
-    }
-}
-
-// Parameter gradients: sums over the sequences, a thread per (channel, value).
-__global__ __launch_bounds__(64) void scan_par_kernel(ScanArgs a, int64_t n_rows) {
-    const int n_state = a.cfg.n_state;
-    const int64_t i = (int64_t)blockIdx.x * 64 + threadIdx.x, width = (int64_t)a.cfg.dim * (n_state + 2);
-    if (i >= width) return;
-    const float* par = back_ws(a.cfg, a.ws, n_rows).par + i;
-    float acc = 0.f;
-    for (int q = 0; q < a.rows.n_seq; ++q) acc += par[q * width];
-    const int64_t d = i / (n_state + 2);
-    const int k = (int)(i % (n_state + 2));
-    if (k < n_state) {
-        if (a.grad.da) a.grad.da[d * n_state + k] = acc;
-    } else if (k == n_state) {
-        if (a.grad.dskip) a.grad.dskip[d] = acc;
-    } else if (a.grad.ddelta_bias) {
-        a.grad.ddelta_bias[d] = acc;
+        if (out.data) row_out<T>(out, r)[group * n_state + (k < n_state ? k : k - n_state)] = (T)acc;
     }
 }
 
@@ -361,7 +606,7 @@ int scan_tiles(const aug_scan_cfg& cfg) {
 }
 
 int scan_lg_block(const aug_scan_cfg& cfg, int n_seq, const int64_t* begin, const int64_t* lengths, int n_cu, bool backward) {
-    if (backward) return 30;
+    if (backward) return cfg.n_state <= 64 ? 5 : 4;      // BackTile
     // A row of a group's channels takes some 150 cycles of each of its four SIMDs; a sequence in one piece takes no less than its
     // length of them.  In blocks the walk is done nearly twice (end states, then outputs), with a launch and the joining between.
     int64_t rows = 0, longest = 0;
@@ -376,9 +621,27 @@ int scan_lg_block(const aug_scan_cfg& cfg, int n_seq, const int64_t* begin, cons
     while (lg > 6 && (rows >> lg) * tiles < 4 * (int64_t)n_cu) --lg;
     return lg;
 }
-size_t scan_workspace(const aug_scan_cfg& cfg, int n_items, int64_t n_rows, int, bool backward) {
+// The gradients' lanes: at least four per channel, so that a block's elements are eight to a lane at most.
+template <class F> hipError_t with_back_lanes(int n_state, F f) {
+    using std::integral_constant;
+    if (n_state <= 8) return f(integral_constant<int, 4>(), integral_constant<int, 2>());
+    if (n_state <= 16) return f(integral_constant<int, 4>(), integral_constant<int, 4>());
+    if (n_state <= 32) return f(integral_constant<int, 8>(), integral_constant<int, 4>());
+    if (n_state <= 64) return f(integral_constant<int, 8>(), integral_constant<int, 8>());
+    return f(integral_constant<int, 16>(), integral_constant<int, 8>());
+}
+BackPlan back_plan(const aug_scan_cfg& cfg, int n_items, int n_cu) {
+    const int cw = 256 / (cfg.n_state <= 16 ? 4 : cfg.n_state <= 64 ? 8 : 16);
+    BackPlan p;
+    p.tiles = cfg.n_group * ((cfg.dim / cfg.n_group + cw - 1) / cw);
+    const int64_t runs = (8 * (int64_t)n_cu + p.tiles - 1) / p.tiles;
+    p.runs = (int)(runs < n_items ? runs : n_items);
+    return p;
+}
+size_t scan_workspace(const aug_scan_cfg& cfg, int n_items, int64_t n_rows, int n_cu, bool backward) {
     if (!backward) return 4 * (size_t)n_items * cfg.dim * (cfg.n_state + 1);      // first states, steps' sums
-    return 4 * ((size_t)n_rows * cfg.dim * cfg.n_state + (size_t)tiles_of(cfg) * n_rows * 2 * cfg.n_state + (size_t)n_items * cfg.dim * (cfg.n_state + 2));
+    const BackPlan p = back_plan(cfg, n_items, n_cu);
+    return 4 * ((size_t)n_items * cfg.dim * (2 * cfg.n_state + 1) + (size_t)p.tiles * n_rows * 2 * cfg.n_state + (size_t)p.runs * cfg.dim * (cfg.n_state + 2));
 }
 
 hipError_t launch_scan(hipStream_t s, const ScanArgs& a, int) {
@@ -418,22 +681,34 @@ hipError_t launch_scan_step(hipStream_t s, int n_seq, const ScanArgs& a, int n_c
     });
 }
 
-hipError_t launch_scan_backward(hipStream_t s, const ScanArgs& a, int64_t n_rows, int) {
-    return with_type(a.cfg.dtype, [&](auto t) {
-        using T = decltype(t);
-        scan_backward_kernel<T><<<dim3((unsigned)a.rows.n_seq, (unsigned)tiles_of(a.cfg)), dim3(kChannels), 8 * kChannels * a.cfg.n_state, s>>>(a, n_rows);
-        hipError_t e = hipGetLastError();
-        if (e == hipSuccess && (a.grad.db.data || a.grad.dc.data)) {
-            scan_bc_kernel<T><<<dim3((unsigned)a.rows.n_seq), dim3(256), 0, s>>>(a, n_rows);
-            e = hipGetLastError();
-        }
-        const int64_t width = (int64_t)a.cfg.dim * (a.cfg.n_state + 2);
-        if (e == hipSuccess && (a.grad.da || a.grad.dskip || a.grad.ddelta_bias)) {
-            scan_par_kernel<<<dim3((unsigned)((width + 63) / 64)), dim3(64), 0, s>>>(a, n_rows);
-            e = hipGetLastError();
-        }
-        return e;
+hipError_t launch_scan_backward(hipStream_t s, const ScanArgs& a, int64_t n_rows, int n_cu) {
+    const BackPlan plan = back_plan(a.cfg, a.rows.n_items, n_cu);
+    BackWs ws = back_ws(a.cfg, a.ws, a.rows.n_items, n_rows, plan.tiles);
+    const int64_t dim = a.cfg.dim, width = dim * a.cfg.n_state, stride = width + 2 * dim;
+    if (!a.grad.da && !a.grad.dskip && !a.grad.ddelta_bias) ws.par = nullptr;
+    const bool joined = a.rows.n_items > a.rows.n_seq;   // a sequence of more than one block
+    hipError_t e = with_type(a.cfg.dtype, [&](auto t) {
+        return with_back_lanes(a.cfg.n_state, [&](auto ln, auto k) {
+            using T = decltype(t);
+            if (joined) {
+                scan_back_sums_kernel<T, ln.value, k.value><<<dim3((unsigned)plan.tiles, (unsigned)a.rows.n_items), dim3(256), 0, s>>>(a, ws);
+                hipError_t e = hipGetLastError();
+                if (e != hipSuccess) return e;
+                scan_back_join_kernel<<<dim3((unsigned)((width + 63) / 64), (unsigned)a.rows.n_seq), dim3(64), 0, s>>>(a, ws);
+                e = hipGetLastError();
+                if (e != hipSuccess) return e;
+            }
+            scan_back_kernel<T, ln.value, k.value><<<dim3((unsigned)(plan.tiles * plan.runs)), dim3(256), 0, s>>>(a, ws, plan, n_rows, joined);
+            hipError_t e = hipGetLastError();
+            if (e != hipSuccess || (!a.grad.db.data && !a.grad.dc.data)) return e;
+            scan_bc_kernel<T><<<dim3((unsigned)a.rows.n_items), dim3(256), 0, s>>>(a, ws, plan, n_rows);
+            return hipGetLastError();
+        });
     });
+    if (e == hipSuccess && a.grad.da) e = launch_sum_partials(s, ws.par, plan.runs, stride, width, a.grad.da);
+    if (e == hipSuccess && a.grad.dskip) e = launch_sum_partials(s, ws.par + width, plan.runs, stride, dim, a.grad.dskip);
+    if (e == hipSuccess && a.grad.ddelta_bias) e = launch_sum_partials(s, ws.par + width + dim, plan.runs, stride, dim, a.grad.ddelta_bias);
+    return e;
 }
 
 }  // namespace aug
