@@ -74,22 +74,41 @@ __global__ __launch_bounds__(64) void norm_backward_kernel(NormBackArgs a) {
     }
 }
 
+// 64 columns to a group, every fourth row a wavefront's, eight rows' loads on their way at once (one row after another took 38 us for
+// 128 rows).
 constexpr int kColumns = 64;
-__global__ __launch_bounds__(kColumns) void sum_partials_kernel(const float* partial, int n_partial, int64_t stride, int64_t width, float* out) {
-    const int64_t c = (int64_t)blockIdx.x * kColumns + threadIdx.x;
-    if (c >= width) return;
+__global__ __launch_bounds__(4 * kColumns) void sum_partials_kernel(const float* partial, int n_partial, int64_t stride, SumOuts outs) {
+    __shared__ float part[4][kColumns];
+    const int lane = threadIdx.x % kColumns, wave = threadIdx.x / kColumns;
+    const int64_t c = (int64_t)blockIdx.x * kColumns + lane, width = outs.part[0].width + outs.part[1].width + outs.part[2].width;
+    constexpr int kAhead = 8;
     float acc = 0.f;
-    for (int p = 0; p < n_partial; ++p) acc += partial[p * stride + c];
-    out[c] = acc;
+    for (int p = wave; p < n_partial; p += 4 * kAhead) {
+        float v[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) v[j] = c < width && p + 4 * j < n_partial ? partial[(p + 4 * j) * stride + c] : 0.f;
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) acc += v[j];
+    }
+    part[wave][lane] = acc;
+    __syncthreads();
+    if (wave || c >= width) return;
+    const float sum = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
+    int64_t at = c;
+    for (const SumOuts::Out& o : outs.part) {
+        if (at >= 0 && at < o.width && o.out) o.out[at] = sum;
+        at -= o.width;
+    }
 }
 
 int rows_per_partial(int64_t n_rows) { return (int)((n_rows + 1023) / 1024 < 64 ? 64 : (n_rows + 1023) / 1024); }
 
 }  // namespace
 
-hipError_t launch_sum_partials(hipStream_t s, const float* partial, int n_partial, int64_t stride, int64_t width, float* out) {
+hipError_t launch_sum_partials(hipStream_t s, const float* partial, int n_partial, int64_t stride, const SumOuts& outs) {
+    const int64_t width = outs.part[0].width + outs.part[1].width + outs.part[2].width;
     if (width <= 0) return hipSuccess;
-    sum_partials_kernel<<<dim3((unsigned)((width + kColumns - 1) / kColumns)), dim3(kColumns), 0, s>>>(partial, n_partial, stride, width, out);
+    sum_partials_kernel<<<dim3((unsigned)((width + kColumns - 1) / kColumns)), dim3(4 * kColumns), 0, s>>>(partial, n_partial, stride, outs);
     return hipGetLastError();
 }
 
@@ -109,7 +128,7 @@ hipError_t launch_norm_backward(hipStream_t s, const NormBackArgs& a, int n_cu) 
             norm_dweight_kernel<decltype(t)><<<dim3((unsigned)((a.dim + 63) / 64), (unsigned)n), dim3(64), 0, s>>>(a, rows_per_partial(a.n_rows));
             hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
-            e = launch_sum_partials(s, a.partial, n, a.dim, a.dim, a.dweight);
+            e = launch_sum_partials(s, a.partial, n, a.dim, {{{a.dweight, a.dim}, {}, {}}});
             if (e != hipSuccess) return e;
         }
         if (a.dx.data) norm_backward_kernel<decltype(t)><<<dim3((unsigned)a.n_rows), dim3(64), 0, s>>>(a);

@@ -317,7 +317,7 @@ int aug_rms_norm_backward_batch(aug_ctx* ctx, int64_t n_rows, const aug_norm_cfg
         sp.add("dweight_out", dweight_out, 0, 4 * (int64_t)cfg->dim, 1, 1, 0);
         AUG_TRY(sp.check(ctx));
         if (n_rows == 0) {
-            if (dweight_out) AUG_HIP(aug::launch_sum_partials(ctx->stream, nullptr, 0, 0, cfg->dim, dweight_out), "gradient sum kernel");
+            if (dweight_out) AUG_HIP(aug::launch_sum_partials(ctx->stream, nullptr, 0, 0, {{{dweight_out, cfg->dim}, {}, {}}}), "gradient sum kernel");
             return AUG_OK;
         }
         if (!a.dx.data && !dweight_out) return AUG_OK;
@@ -403,8 +403,8 @@ int aug_short_conv_backward_batch(aug_ctx* ctx, int n_seq, const int64_t* row_of
         AUG_TRY(sp.check(ctx));
         if (!a.dx.data && !dweight_out && !dbias_out) return AUG_OK;
         if (seq.total == 0) {
-            if (dweight_out) AUG_HIP(aug::launch_sum_partials(ctx->stream, nullptr, 0, 0, (int64_t)cfg->dim * cfg->taps, dweight_out), "gradient sum kernel");
-            if (dbias_out) AUG_HIP(aug::launch_sum_partials(ctx->stream, nullptr, 0, 0, cfg->dim, dbias_out), "gradient sum kernel");
+            const aug::SumOuts zeros{{{dweight_out, (int64_t)cfg->dim * cfg->taps}, {dbias_out, cfg->dim}, {}}};
+            AUG_HIP(aug::launch_sum_partials(ctx->stream, nullptr, 0, 0, zeros), "gradient sum kernel");
             return AUG_OK;
         }
         AUG_TRY(seq.plan(aug::short_conv_lg_block(*cfg, true)));
@@ -525,9 +525,8 @@ int aug_scan_backward_batch(aug_ctx* ctx, int n_seq, const int64_t* row_offsets,
         AUG_TRY(sp.check(ctx));
         if (!any) return AUG_OK;
         if (seq.total == 0) {
-            if (g.da) AUG_HIP(aug::launch_sum_partials(ctx->stream, nullptr, 0, 0, (int64_t)cfg->dim * cfg->n_state, g.da), "gradient sum kernel");
-            if (g.dskip) AUG_HIP(aug::launch_sum_partials(ctx->stream, nullptr, 0, 0, cfg->dim, g.dskip), "gradient sum kernel");
-            if (g.ddelta_bias) AUG_HIP(aug::launch_sum_partials(ctx->stream, nullptr, 0, 0, cfg->dim, g.ddelta_bias), "gradient sum kernel");
+            const aug::SumOuts zeros{{{g.da, (int64_t)cfg->dim * cfg->n_state}, {g.dskip, cfg->dim}, {g.ddelta_bias, cfg->dim}}};
+            AUG_HIP(aug::launch_sum_partials(ctx->stream, nullptr, 0, 0, zeros), "gradient sum kernel");
             return AUG_OK;
         }
         AUG_TRY(seq.plan(aug::scan_lg_block(*cfg, n_seq, row_offsets, row_lengths, ctx->n_cu, true)));

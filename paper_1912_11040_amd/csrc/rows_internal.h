@@ -14,8 +14,15 @@ struct RowBlocks {
     const int2* items = nullptr;         // device [n_items]: (sequence, block of it)
 };
 
-// out[c] = sum over p < n_partial of partial[p * stride + c], c < width; in that order, so that the result has one value.
-hipError_t launch_sum_partials(hipStream_t s, const float* partial, int n_partial, int64_t stride, int64_t width, float* out);
+// Sums of the columns of partial [n_partial][stride] into up to three arrays that follow one another in a row of it (null: not wanted).
+// The terms of a column are added in an order that depends on n_partial only.
+struct SumOuts {
+    struct Out {
+        float* out;
+        int64_t width;
+    } part[3];
+};
+hipError_t launch_sum_partials(hipStream_t s, const float* partial, int n_partial, int64_t stride, const SumOuts& outs);
 
 struct NormArgs {
     int64_t n_rows;

@@ -234,7 +234,7 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, int n_seq, i
 // before each block and of R what comes in from behind.  With both the blocks are independent of one another: the main pass
 // walks a block forward for its states and back for its gradients, in stretches of SUB rows whose states and decays stay in registers.
 template <int LN, int K> struct BackTile {
-    static constexpr int CW = 256 / LN, NP = LN * K, LG = NP <= 64 ? 5 : 4, RT = 1 << LG, EPT = RT * CW / 256, SUB = K <= 4 ? 16 : 8;
+    static constexpr int CW = 256 / LN, NP = LN * K, LG = NP <= 64 ? 5 : 4, RT = 1 << LG, EPT = RT * CW / 256, SUB = K <= 2 ? 16 : 8;
     static constexpr int BC = (RT * NP + 255) / 256;
 };
 
@@ -373,7 +373,7 @@ __global__ __launch_bounds__(64) void scan_back_join_kernel(ScanArgs a, BackWs w
 }
 
 template <class T, int LN, int K>
-__global__ __launch_bounds__(256) void scan_back_kernel(ScanArgs a, BackWs ws, BackPlan plan, int64_t n_rows, bool joined) {
+__global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs a, BackWs ws, BackPlan plan, int64_t n_rows, bool joined) {
     using G = BackTile<LN, K>;
     constexpr int NS = G::RT / G::SUB, V = 2 * K;
     __shared__ float2 su[G::RT][G::CW];                  // (step, step u); behind a row's walk (sum g b, sum of e g h a)
@@ -705,9 +705,7 @@ hipError_t launch_scan_backward(hipStream_t s, const ScanArgs& a, int64_t n_rows
             return hipGetLastError();
         });
     });
-    if (e == hipSuccess && a.grad.da) e = launch_sum_partials(s, ws.par, plan.runs, stride, width, a.grad.da);
-    if (e == hipSuccess && a.grad.dskip) e = launch_sum_partials(s, ws.par + width, plan.runs, stride, dim, a.grad.dskip);
-    if (e == hipSuccess && a.grad.ddelta_bias) e = launch_sum_partials(s, ws.par + width + dim, plan.runs, stride, dim, a.grad.ddelta_bias);
+    if (e == hipSuccess && ws.par) e = launch_sum_partials(s, ws.par, plan.runs, stride, {{{a.grad.da, width}, {a.grad.dskip, dim}, {a.grad.ddelta_bias, dim}}});
     return e;
 }
 

@@ -116,8 +116,7 @@ hipError_t launch_short_conv_backward(hipStream_t s, const ShortConvArgs& a, int
         return hipGetLastError();
     });
     const int64_t w = (int64_t)a.cfg.dim * a.cfg.taps, stride = w + a.cfg.dim;
-    if (e == hipSuccess && a.dweight) e = launch_sum_partials(s, a.partial, a.rows.n_items, stride, w, a.dweight);
-    if (e == hipSuccess && a.dbias) e = launch_sum_partials(s, a.partial + w, a.rows.n_items, stride, a.cfg.dim, a.dbias);
+    if (e == hipSuccess && a.partial) e = launch_sum_partials(s, a.partial, a.rows.n_items, stride, {{{a.dweight, w}, {a.dbias, a.cfg.dim}, {}}});
     return e;
 }
 
