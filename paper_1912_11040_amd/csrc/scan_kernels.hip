@@ -268,6 +268,24 @@ template <int BIT, int N, int V> __device__ inline void halve(float (&v)[V]) {
     }
 }
 
+// Sums of 2 EPT values over the lanes of a wavefront that are APART apart (they hold the same channels of other rows).  The sums are
+// dealt to these lanes: lane l keeps kept<EPT>() of them, from value kept_from<EPT>(l) on.
+template <int EPT> __host__ __device__ constexpr int kept() { return EPT >= 2 ? EPT / 2 : 1; }
+template <int EPT> __device__ inline int kept_from(int lane) { return EPT >= 2 ? ((lane >> 5) * 2 + (lane >> 4 & 1)) * (EPT / 2) : lane >> 5; }
+template <int APART, int EPT> __device__ inline void sum_rows(float (&v)[2 * EPT]) {
+    static_assert((APART == 8 && EPT >= 2) || (APART == 16 && EPT == 1), "the tiles' layouts");
+    halve<5, 2 * EPT>(v);
+    if constexpr (EPT >= 2) {
+        halve<4, EPT>(v);
+#pragma unroll
+        for (int i = 0; i < EPT / 2; ++i) v[i] = dpp_add<0x128>(v[i]);
+    } else {
+        const unsigned x = __float_as_uint(v[0]);
+        const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+        v[0] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+}
+
 template <class T, int LN, int K>
 __global__ __launch_bounds__(256) void scan_back_sums_kernel(ScanArgs a, BackWs ws) {
     using G = BackTile<LN, K>;
@@ -372,6 +390,21 @@ __global__ __launch_bounds__(64) void scan_back_join_kernel(ScanArgs a, BackWs w
     }
 }
 
+// What a walker reads of a row: its channel's step, step u and dp, its states' b or c.  Rows are read one ahead of their use: the
+// scheduler would otherwise put a row's reads right before it and wait for LDS at every row.
+template <int K> struct RowIn {
+    float2 s;
+    float dp, v[K];
+    template <int R, int CW, int NP>
+    __device__ inline void load(const float2 (&su)[R][CW], const float (&sdp)[R][CW], const float (&sv)[R][NP], int t, int ch, int nq) {
+        s = su[t][ch];
+        dp = sdp[t][ch];
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] = sv[t][nq + k];
+    }
+};
+__device__ inline void stay_ahead() { __builtin_amdgcn_sched_barrier(0x2 | 0x4 | 0x200); }      // arithmetic and LDS writes may pass, reads not
+
 template <class T, int LN, int K>
 __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs a, BackWs ws, BackPlan plan, int64_t n_rows, bool joined) {
     using G = BackTile<LN, K>;
@@ -380,6 +413,7 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
     __shared__ float sdp[G::RT][G::CW];                  // dp; behind a row's walk sum c h
     __shared__ float sb[G::RT][G::NP], sc[G::RT][G::NP];
     __shared__ float sbc[4][G::RT][2 * G::NP];           // each wavefront's sums over its channels for db and dc
+    __shared__ float sbias[G::CW], sskip[G::CW];
     const int tid = threadIdx.x, dim = a.cfg.dim, n_state = a.cfg.n_state, per_group = dim / a.cfg.n_group;
     const int tile = blockIdx.x % plan.tiles, run = blockIdx.x / plan.tiles;
     const int tiles = plan.tiles / a.cfg.n_group, group = tile / tiles, in_group = (tile % tiles) * G::CW;
@@ -392,13 +426,13 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
 #pragma unroll
     for (int k = 0; k < K; ++k) rate[k] = walks && nq + k < n_state ? rate2(a.in.a[(int64_t)(d0 + ch) * n_state + nq + k]) : 0.f;
     const int lt = tid / (G::CW / G::EPT), lc = tid % (G::CW / G::EPT) * G::EPT;
-    float bias[G::EPT], skip[G::EPT], dskip[G::EPT] = {}, dbias[G::EPT] = {};
-#pragma unroll
-    for (int i = 0; i < G::EPT; ++i) {
-        bias[i] = a.in.delta_bias && lc + i < width ? a.in.delta_bias[d0 + lc + i] : 0.f;
-        skip[i] = a.in.skip && lc + i < width ? a.in.skip[d0 + lc + i] : 0.f;
+    if (tid < G::CW) {
+        sbias[tid] = a.in.delta_bias && tid < width ? a.in.delta_bias[d0 + tid] : 0.f;
+        sskip[tid] = a.in.skip && tid < width ? a.in.skip[d0 + tid] : 0.f;
     }
+    float acc[kept<G::EPT>()] = {};                      // dskip and ddelta_bias, as sum_rows deals them
     const bool gate = a.in.z.data;
+    __syncthreads();
 
     for (int it = first_item; it < end_item; ++it) {
         const int2 item = a.rows.items[it];
@@ -435,7 +469,7 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
         float step[G::EPT];
 #pragma unroll
         for (int i = 0; i < G::EPT; ++i) {
-            step[i] = i < valid ? step_of(a.cfg, (float)delta.v[i] + bias[i]) : 0.f;
+            step[i] = i < valid ? step_of(a.cfg, (float)delta.v[i] + sbias[lc + i]) : 0.f;
             su[lt][lc + i] = make_float2(step[i], step[i] * (float)u.v[i]);
             float dp = (float)dy.v[i];
             if (gate) dp *= (float)z.v[i] * sigmoid((float)z.v[i]);
@@ -462,34 +496,44 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
             float h[G::SUB + 1][K], e[G::SUB][K];
 #pragma unroll
             for (int k = 0; k < K; ++k) h[0][k] = st[s][k];
+            RowIn<K> next;
+            next.load(su, sdp, sb, s * G::SUB, ch, nq);
 #pragma unroll
             for (int j = 0; j < G::SUB; ++j) {
-                const int t = s * G::SUB + j;
-                const float2 x = su[t][ch];
+                const RowIn<K> x = next;
+                if (j + 1 < G::SUB) next.load(su, sdp, sb, s * G::SUB + j + 1, ch, nq);
+                stay_ahead();
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
-                    e[j][k] = __builtin_amdgcn_exp2f(x.x * rate[k]);
-                    h[j + 1][k] = fmaf(e[j][k], h[j][k], x.y * sb[t][nq + k]);
+                    e[j][k] = __builtin_amdgcn_exp2f(x.s.x * rate[k]);
+                    h[j + 1][k] = fmaf(e[j][k], h[j][k], x.s.y * x.v[k]);
                 }
             }
             float keep_gb = 0.f, keep_eh = 0.f, keep_p = 0.f;
+            RowIn<K> next_c;
+            next.load(su, sdp, sb, (s + 1) * G::SUB - 1, ch, nq);
+            next_c.load(su, sdp, sc, (s + 1) * G::SUB - 1, ch, nq);
 #pragma unroll
             for (int j = G::SUB - 1; j >= 0; --j) {
                 const int t = s * G::SUB + j;
-                const float2 x = su[t][ch];
-                const float dp = sdp[t][ch];
+                const RowIn<K> x = next, xc = next_c;
+                if (j > 0) {
+                    next.load(su, sdp, sb, t - 1, ch, nq);
+                    next_c.load(su, sdp, sc, t - 1, ch, nq);
+                }
+                stay_ahead();
                 float gb = 0.f, eha = 0.f, p = 0.f, v[V];
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
-                    const float c = sc[t][nq + k], g = fmaf(c, dp, carried[k]);
+                    const float c = xc.v[k], g = fmaf(c, x.dp, carried[k]);
                     carried[k] = e[j][k] * g;
                     const float eh = carried[k] * h[j][k];
                     p = fmaf(c, h[j + 1][k], p);
-                    gb = fmaf(g, sb[t][nq + k], gb);
+                    gb = fmaf(g, x.v[k], gb);
                     eha = fmaf(eh, rate[k], eha);
-                    da[k] = fmaf(eh, x.x, da[k]);
-                    v[k] = g * x.y;
-                    v[K + k] = dp * h[j + 1][k];
+                    da[k] = fmaf(eh, x.s.x, da[k]);
+                    v[k] = g * x.s.y;
+                    v[K + k] = x.dp * h[j + 1][k];
                 }
                 gb = lanes_sum<LN>(gb);
                 eha = lanes_sum<LN>(eha);
@@ -530,24 +574,31 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
             }
         }
         __syncthreads();
+        float par[2 * G::EPT];                           // the row's dskip, then its ddelta_bias
+        Pack<T, G::EPT> du, dd, dz;
 #pragma unroll
         for (int i = 0; i < G::EPT; ++i) {
-            if (i >= valid) break;
             const float2 x = su[lt][lc + i];
-            const float ui = (float)u.v[i], raw = (float)delta.v[i] + bias[i], dyi = (float)dy.v[i];
+            const float ui = (float)u.v[i], dyi = (float)dy.v[i], skip = sskip[lc + i];
             float dp = dyi;
             if (gate) {
                 const float zi = (float)z.v[i], sg = sigmoid(zi);
                 dp = dyi * zi * sg;
-                if (a.grad.dz.data) row_out<T>(a.grad.dz, r)[d0 + lc + i] = (T)(dyi * fmaf(skip[i], ui, sdp[lt][lc + i]) * sg * (1.f + zi * (1.f - sg)));
+                dz.v[i] = (T)(dyi * fmaf(skip, ui, sdp[lt][lc + i]) * sg * (1.f + zi * (1.f - sg)));
             }
-            const float dstep = fmaf(ui, x.x, x.y * 0.693147180559945309f);      // (the rates are those of powers of two)
-            const float dd = a.cfg.softplus ? dstep * sigmoid(raw) : dstep;
-            if (a.grad.du.data) row_out<T>(a.grad.du, r)[d0 + lc + i] = (T)fmaf(step[i], x.x, skip[i] * dp);
-            if (a.grad.ddelta.data) row_out<T>(a.grad.ddelta, r)[d0 + lc + i] = (T)dd;
-            dskip[i] = fmaf(dp, ui, dskip[i]);
-            dbias[i] += dd;
+            float dstep = fmaf(ui, x.x, x.y * 0.693147180559945309f);      // (the rates are those of powers of two)
+            if (a.cfg.softplus) dstep *= sigmoid((float)delta.v[i] + sbias[lc + i]);
+            du.v[i] = (T)fmaf(step[i], x.x, skip * dp);
+            dd.v[i] = (T)dstep;
+            par[i] = i < valid ? dp * ui : 0.f;
+            par[G::EPT + i] = i < valid ? dstep : 0.f;
         }
+        if (a.grad.du.data) store_pack<T, G::EPT>(row_out<T>(a.grad.du, r) + d0 + lc, du, valid);
+        if (a.grad.ddelta.data) store_pack<T, G::EPT>(row_out<T>(a.grad.ddelta, r) + d0 + lc, dd, valid);
+        if (a.grad.dz.data) store_pack<T, G::EPT>(row_out<T>(a.grad.dz, r) + d0 + lc, dz, valid);
+        sum_rows<G::CW / G::EPT, G::EPT>(par);
+#pragma unroll
+        for (int i = 0; i < kept<G::EPT>(); ++i) acc[i] += par[i];
         for (int e = tid; e < here * 2 * n_state; e += 256) {
             const int t = e / (2 * n_state), n = e % (2 * n_state), at = n < n_state ? n : n - n_state + G::NP;
             ws.bc[((int64_t)tile * n_rows + begin + t) * 2 * n_state + n] = (sbc[0][t][at] + sbc[1][t][at]) + (sbc[2][t][at] + sbc[3][t][at]);
@@ -559,15 +610,20 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
 #pragma unroll
     for (int k = 0; k < K; ++k)
         if (walks && nq + k < n_state) par[(int64_t)(d0 + ch) * n_state + nq + k] = da[k];
-    // over the rows of the tile, first to last
+    // each wavefront's sums, then theirs
+    float* const sums = &sdp[0][0];                      // [4][2][CW]
+    if (tid % (2 * G::CW / G::EPT) < G::CW / G::EPT) {
 #pragma unroll
-    for (int i = 0; i < G::EPT; ++i) su[lt][lc + i] = make_float2(dskip[i], dbias[i]);
+        for (int i = 0; i < kept<G::EPT>(); ++i) {
+            const int val = kept_from<G::EPT>(tid % 64) + i;
+            sums[(wave * 2 + val / G::EPT) * G::CW + lc + val % G::EPT] = acc[i];
+        }
+    }
     __syncthreads();
     if (tid >= width) return;
-    float ds = 0.f, db = 0.f;
-    for (int t = 0; t < G::RT; ++t) ds += su[t][tid].x, db += su[t][tid].y;
-    par[(int64_t)dim * n_state + d0 + tid] = ds;
-    par[(int64_t)dim * (n_state + 1) + d0 + tid] = db;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+        par[(int64_t)dim * (n_state + j) + d0 + tid] = (sums[j * G::CW + tid] + sums[(2 + j) * G::CW + tid]) + (sums[(4 + j) * G::CW + tid] + sums[(6 + j) * G::CW + tid]);
 }
 
 // db and dc: sums over the tiles of a group, a group of threads per block of rows.
