@@ -8,6 +8,16 @@ namespace aug {
 namespace {
 
 __device__ inline float step_of(const aug_scan_cfg& cfg, float v) { return cfg.softplus ? softplus(v) : v; }
+// Steps of N elements.  (The choice is the call's: made once, not per element, the elements' exponentials overlap.)
+template <int N> __device__ inline void steps_of(const aug_scan_cfg& cfg, const float (&raw)[N], float (&step)[N]) {
+    if (cfg.softplus) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) step[i] = softplus(raw[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) step[i] = raw[i];
+    }
+}
 // The rate for powers of two, finite also for the lowest numbers: a step of zero keeps the state.
 __device__ inline float rate2(float a) {
     const float r = a * kLog2e;
@@ -84,12 +94,14 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, float* first_stat
     if (rows > 0) fetch(0);
     for (int t0 = 0; t0 < rows; t0 += G::TT) {
         const int here = min(G::TT, rows - t0);
-        float us[G::EPT];
+        float us[G::EPT], raw[G::EPT], step[G::EPT];
+#pragma unroll
+        for (int i = 0; i < G::EPT; ++i) raw[i] = (float)delta.v[i] + bias[i];
+        steps_of(a.cfg, raw, step);
 #pragma unroll
         for (int i = 0; i < G::EPT; ++i) {
             us[i] = (float)u.v[i];
-            const float step = step_of(a.cfg, (float)delta.v[i] + bias[i]);
-            if (lt < here) su[lt][lc + i] = make_float2(step, step * us[i]);
+            su[lt][lc + i] = make_float2(step[i], step[i] * us[i]);      // (rows behind the block are not walked)
         }
         const Pack<T, G::EPT> zs = z;
 #pragma unroll
@@ -135,15 +147,15 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, float* first_stat
         __syncthreads();
         if (MODE != kSums && lt < here) {
             Pack<T, G::EPT> out;
+            float p[G::EPT];
 #pragma unroll
-            for (int i = 0; i < G::EPT; ++i) {
-                float p = fmaf(skip[i], us[i], sy[lt][lc + i]);
-                if (gate) {
-                    const float g = (float)zs.v[i];
-                    p *= g * sigmoid(g);
-                }
-                out.v[i] = (T)p;
+            for (int i = 0; i < G::EPT; ++i) p[i] = fmaf(skip[i], us[i], sy[lt][lc + i]);
+            if (gate) {
+#pragma unroll
+                for (int i = 0; i < G::EPT; ++i) p[i] *= (float)zs.v[i] * sigmoid((float)zs.v[i]);
             }
+#pragma unroll
+            for (int i = 0; i < G::EPT; ++i) out.v[i] = (T)p[i];
             store_pack<T, G::EPT>(row_out<T>(a.y, begin + t0 + lt) + d0 + lc, out, valid);
         }
     }
@@ -315,13 +327,21 @@ __global__ __launch_bounds__(256) void scan_back_sums_kernel(ScanArgs a, BackWs 
         sb[t][n] = there ? (float)row_in<T>(a.in.b, begin + t)[col] : 0.f;
         sc[t][n] = there ? (float)row_in<T>(a.in.c, begin + t)[col] : 0.f;
     }
+    float raw[G::EPT], step[G::EPT], dp[G::EPT];
 #pragma unroll
     for (int i = 0; i < G::EPT; ++i) {
-        const float step = i < valid ? step_of(a.cfg, (float)delta.v[i] + (a.in.delta_bias ? a.in.delta_bias[d0 + lc + i] : 0.f)) : 0.f;
-        su[lt][lc + i] = make_float2(step, step * (float)u.v[i]);
-        float dp = (float)dy.v[i];
-        if (a.in.z.data) dp *= (float)z.v[i] * sigmoid((float)z.v[i]);
-        sdp[lt][lc + i] = dp;
+        raw[i] = (float)delta.v[i] + (a.in.delta_bias && i < valid ? a.in.delta_bias[d0 + lc + i] : 0.f);
+        dp[i] = (float)dy.v[i];
+    }
+    steps_of(a.cfg, raw, step);
+    if (a.in.z.data) {
+#pragma unroll
+        for (int i = 0; i < G::EPT; ++i) dp[i] *= (float)z.v[i] * sigmoid((float)z.v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < G::EPT; ++i) {                   // (neither rows behind the block nor channels behind the tile are walked)
+        su[lt][lc + i] = make_float2(step[i], step[i] * (float)u.v[i]);
+        sdp[lt][lc + i] = dp[i];
     }
     __syncthreads();
     const int ch = tid / LN, nq = (tid % LN) * K;
@@ -414,6 +434,7 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
     __shared__ float sb[G::RT][G::NP], sc[G::RT][G::NP];
     __shared__ float sbc[4][G::RT][2 * G::NP];           // each wavefront's sums over its channels for db and dc
     __shared__ float sbias[G::CW], sskip[G::CW];
+    __shared__ float sst[NS][256][K];                    // each lane's states before the stretches
     const int tid = threadIdx.x, dim = a.cfg.dim, n_state = a.cfg.n_state, per_group = dim / a.cfg.n_group;
     const int tile = blockIdx.x % plan.tiles, run = blockIdx.x / plan.tiles;
     const int tiles = plan.tiles / a.cfg.n_group, group = tile / tiles, in_group = (tile % tiles) * G::CW;
@@ -434,68 +455,117 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
     const bool gate = a.in.z.data;
     __syncthreads();
 
-    for (int it = first_item; it < end_item; ++it) {
+    // A block's rows and what a lane reads of them.  The next block's are asked for behind the walk, when the states' registers are
+    // free, and where it lies a block earlier.
+    struct Block {
+        int seq, here;
+        int64_t begin;
+    };
+    struct Data {
+        Pack<T, G::EPT> u, delta, dy, z;
+        T b[G::BC], c[G::BC];
+        float first[K], behind[K];
+    };
+    auto locate = [&](int it) -> Block {
+        if (it >= end_item) return {0, 0, 0};
         const int2 item = a.rows.items[it];
-        const int64_t from = a.rows.begin[item.x], begin = from + ((int64_t)item.y << G::LG), end = a.rows.end[item.x];
-        const int here = (int)min(end - begin, (int64_t)G::RT);
-        if (here <= 0) continue;                         // (an empty sequence's block)
-        const int valid = lt < here ? width - lc : 0;
-        const int64_t r = begin + lt;
-        const auto u = load_pack<T, G::EPT>(row_in<T>(a.in.u, r) + d0 + lc, valid);
-        const auto delta = load_pack<T, G::EPT>(row_in<T>(a.in.delta, r) + d0 + lc, valid);
-        const auto dy = load_pack<T, G::EPT>(row_in<T>(a.dy, r) + d0 + lc, valid);
-        Pack<T, G::EPT> z;
-        if (gate) z = load_pack<T, G::EPT>(row_in<T>(a.in.z, r) + d0 + lc, valid);
+        const int64_t begin = a.rows.begin[item.x] + ((int64_t)item.y << G::LG);
+        return {item.x, (int)min(a.rows.end[item.x] - begin, (int64_t)G::RT), begin};
+    };
+    auto fetch = [&](const Block& blk, int it, Data& v) {
+        if (blk.here <= 0) return;
+        const int valid = lt < blk.here ? width - lc : 0;
+        const int64_t r = blk.begin + lt;
+        v.u = load_pack<T, G::EPT>(row_in<T>(a.in.u, r) + d0 + lc, valid);
+        v.delta = load_pack<T, G::EPT>(row_in<T>(a.in.delta, r) + d0 + lc, valid);
+        v.dy = load_pack<T, G::EPT>(row_in<T>(a.dy, r) + d0 + lc, valid);
+        if (gate) v.z = load_pack<T, G::EPT>(row_in<T>(a.in.z, r) + d0 + lc, valid);
 #pragma unroll
         for (int j = 0; j < G::BC; ++j) {
             const int e = tid + 256 * j, t = e / G::NP, n = e % G::NP;
-            if (t >= G::RT) break;
-            const bool there = t < here && n < n_state;
+            const bool there = t < blk.here && n < n_state;
             const int64_t col = (int64_t)group * n_state + n;
-            sb[t][n] = there ? (float)row_in<T>(a.in.b, begin + t)[col] : 0.f;
-            sc[t][n] = there ? (float)row_in<T>(a.in.c, begin + t)[col] : 0.f;
+            v.b[j] = there ? row_in<T>(a.in.b, blk.begin + t)[col] : (T)0;
+            v.c[j] = there ? row_in<T>(a.in.c, blk.begin + t)[col] : (T)0;
         }
         // the state before the block, and what comes in from behind it: e g of the row behind
-        float st[NS][K], carried[K];
-        {
-            const int64_t at = ((int64_t)it * dim + d0 + ch) * n_state + nq, in = ((int64_t)item.x * dim + d0 + ch) * n_state + nq;
+        const int64_t at = ((int64_t)it * dim + d0 + ch) * n_state + nq, in = ((int64_t)blk.seq * dim + d0 + ch) * n_state + nq;
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                const bool there = walks && nq + k < n_state;
-                st[0][k] = !there ? 0.f : joined ? ws.first[at + k] : a.state_in ? a.state_in[in + k] : 0.f;
-                carried[k] = there && joined ? ws.behind[at + k] : 0.f;
+        for (int k = 0; k < K; ++k) {
+            const bool there = walks && nq + k < n_state;
+            v.first[k] = !there ? 0.f : joined ? ws.first[at + k] : a.state_in ? a.state_in[in + k] : 0.f;
+            v.behind[k] = there && joined ? ws.behind[at + k] : 0.f;
+        }
+    };
+    Block blk = locate(first_item), next_blk;
+    Data v, next_v;
+    fetch(blk, first_item, v);
+    for (int it = first_item; it < end_item; ++it, blk = next_blk, v = next_v) {
+        next_blk = locate(it + 1);
+        const int here = blk.here;
+        if (here <= 0) {                                 // (an empty sequence's block)
+            fetch(next_blk, it + 1, next_v);
+            continue;
+        }
+        const int valid = lt < here ? width - lc : 0;
+        const int64_t begin = blk.begin, r = begin + lt;
+        const Pack<T, G::EPT> u = v.u, delta = v.delta, dy = v.dy, z = v.z;
+#pragma unroll
+        for (int j = 0; j < G::BC; ++j) {
+            const int e = tid + 256 * j;
+            if (G::RT * G::NP % 256 == 0 || e < G::RT * G::NP) {
+                (&sb[0][0])[e] = (float)v.b[j];
+                (&sc[0][0])[e] = (float)v.c[j];
             }
         }
-        float step[G::EPT];
+        float carried[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            sst[0][tid][k] = v.first[k];
+            carried[k] = v.behind[k];
+        }
+        float raw[G::EPT], step[G::EPT], dp[G::EPT];
 #pragma unroll
         for (int i = 0; i < G::EPT; ++i) {
-            step[i] = i < valid ? step_of(a.cfg, (float)delta.v[i] + sbias[lc + i]) : 0.f;
+            raw[i] = (float)delta.v[i] + sbias[lc + i];
+            dp[i] = (float)dy.v[i];
+        }
+        steps_of(a.cfg, raw, step);
+        if (gate) {
+#pragma unroll
+            for (int i = 0; i < G::EPT; ++i) dp[i] *= (float)z.v[i] * sigmoid((float)z.v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < G::EPT; ++i) {
+            step[i] = i < valid ? step[i] : 0.f;
             su[lt][lc + i] = make_float2(step[i], step[i] * (float)u.v[i]);
-            float dp = (float)dy.v[i];
-            if (gate) dp *= (float)z.v[i] * sigmoid((float)z.v[i]);
-            sdp[lt][lc + i] = dp;
+            sdp[lt][lc + i] = dp[i];
         }
         __syncthreads();
         // states before the later stretches
+        {
+            float st[K];
 #pragma unroll
-        for (int s = 0; s + 1 < NS; ++s) {
+            for (int k = 0; k < K; ++k) st[k] = v.first[k];
+#pragma unroll 1
+            for (int s = 1; s * G::SUB < here; ++s) {
 #pragma unroll
-            for (int k = 0; k < K; ++k) st[s + 1][k] = st[s][k];
-            if ((s + 1) * G::SUB < here) {
-#pragma unroll 4
-                for (int t = s * G::SUB; t < (s + 1) * G::SUB; ++t) {
+                for (int j = 0; j < G::SUB; ++j) {
+                    const int t = (s - 1) * G::SUB + j;
                     const float2 x = su[t][ch];
 #pragma unroll
-                    for (int k = 0; k < K; ++k) st[s + 1][k] = fmaf(__builtin_amdgcn_exp2f(x.x * rate[k]), st[s + 1][k], x.y * sb[t][nq + k]);
+                    for (int k = 0; k < K; ++k) st[k] = fmaf(__builtin_amdgcn_exp2f(x.x * rate[k]), st[k], x.y * sb[t][nq + k]);
                 }
+#pragma unroll
+                for (int k = 0; k < K; ++k) sst[s][tid][k] = st[k];
             }
         }
-#pragma unroll
-        for (int s = NS - 1; s >= 0; --s) {
-            if (s * G::SUB >= here) continue;            // (rows behind the sequence's end inside a stretch have steps and dp of zero)
+        // (rows behind the sequence's end inside a stretch have steps and dp of zero)
+#pragma unroll 1
+        for (int s = (here - 1) / G::SUB; s >= 0; --s) {
             float h[G::SUB + 1][K], e[G::SUB][K];
 #pragma unroll
-            for (int k = 0; k < K; ++k) h[0][k] = st[s][k];
+            for (int k = 0; k < K; ++k) h[0][k] = sst[s][tid][k];
             RowIn<K> next;
             next.load(su, sdp, sb, s * G::SUB, ch, nq);
 #pragma unroll
@@ -522,7 +592,7 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
                     next_c.load(su, sdp, sc, t - 1, ch, nq);
                 }
                 stay_ahead();
-                float gb = 0.f, eha = 0.f, p = 0.f, v[V];
+                float gb = 0.f, eha = 0.f, p = 0.f, w[V];
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
                     const float c = xc.v[k], g = fmaf(c, x.dp, carried[k]);
@@ -532,8 +602,8 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
                     gb = fmaf(g, x.v[k], gb);
                     eha = fmaf(eh, rate[k], eha);
                     da[k] = fmaf(eh, x.s.x, da[k]);
-                    v[k] = g * x.s.y;
-                    v[K + k] = x.dp * h[j + 1][k];
+                    w[k] = g * x.s.y;
+                    w[K + k] = x.dp * h[j + 1][k];
                 }
                 gb = lanes_sum<LN>(gb);
                 eha = lanes_sum<LN>(eha);
@@ -549,12 +619,12 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
                     sdp[t + tid % LN][ch] = keep_p;
                 }
                 // sums over the wavefront's channels (bits log2 LN .. 5 of the lane): a quarter of the values to each 16 lanes
-                halve<5, V>(v);
-                halve<4, V / 2>(v);
+                halve<5, V>(w);
+                halve<4, V / 2>(w);
 #pragma unroll
                 for (int i = 0; i < V / 4; ++i) {
-                    if (LN <= 8) v[i] = dpp_add<0x128>(v[i]);              // lanes eight apart
-                    if (LN <= 4) v[i] = dpp_add<0x124>(v[i]);              // four apart (those eight apart are equal now)
+                    if (LN <= 8) w[i] = dpp_add<0x128>(w[i]);              // lanes eight apart
+                    if (LN <= 4) w[i] = dpp_add<0x124>(w[i]);              // four apart (those eight apart are equal now)
                 }
                 const int lane = tid % 64, quarter = ((lane >> 5) * 2 + (lane >> 4 & 1)) * (V / 4);
                 if (LN <= 8 && V >= 8) {                 // half of them from lanes with bit 3
@@ -562,36 +632,47 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
 #pragma unroll
                     for (int i = 0; i < V / 8; ++i) {
                         const int val = quarter + i + (up ? V / 8 : 0);
-                        sbc[wave][t][val / K * G::NP + nq + val % K] = up ? v[i + V / 8] : v[i];
+                        sbc[wave][t][val / K * G::NP + nq + val % K] = up ? w[i + V / 8] : w[i];
                     }
                 } else {
 #pragma unroll
                     for (int i = 0; i < V / 4; ++i) {
                         const int val = quarter + i;
-                        sbc[wave][t][val / K * G::NP + nq + val % K] = v[i];
+                        sbc[wave][t][val / K * G::NP + nq + val % K] = w[i];
                     }
                 }
             }
         }
         __syncthreads();
+        fetch(next_blk, it + 1, next_v);
         float par[2 * G::EPT];                           // the row's dskip, then its ddelta_bias
         Pack<T, G::EPT> du, dd, dz;
+        float dstep[G::EPT], gb[G::EPT];
 #pragma unroll
         for (int i = 0; i < G::EPT; ++i) {
             const float2 x = su[lt][lc + i];
-            const float ui = (float)u.v[i], dyi = (float)dy.v[i], skip = sskip[lc + i];
-            float dp = dyi;
-            if (gate) {
+            gb[i] = x.x;
+            dstep[i] = fmaf((float)u.v[i], x.x, x.y * 0.693147180559945309f);      // (the rates are those of powers of two)
+            dp[i] = (float)dy.v[i];
+        }
+        if (a.cfg.softplus) {
+#pragma unroll
+            for (int i = 0; i < G::EPT; ++i) dstep[i] *= sigmoid((float)delta.v[i] + sbias[lc + i]);
+        }
+        if (gate) {
+#pragma unroll
+            for (int i = 0; i < G::EPT; ++i) {
                 const float zi = (float)z.v[i], sg = sigmoid(zi);
-                dp = dyi * zi * sg;
-                dz.v[i] = (T)(dyi * fmaf(skip, ui, sdp[lt][lc + i]) * sg * (1.f + zi * (1.f - sg)));
+                dz.v[i] = (T)(dp[i] * fmaf(sskip[lc + i], (float)u.v[i], sdp[lt][lc + i]) * sg * (1.f + zi * (1.f - sg)));
+                dp[i] *= zi * sg;
             }
-            float dstep = fmaf(ui, x.x, x.y * 0.693147180559945309f);      // (the rates are those of powers of two)
-            if (a.cfg.softplus) dstep *= sigmoid((float)delta.v[i] + sbias[lc + i]);
-            du.v[i] = (T)fmaf(step[i], x.x, skip * dp);
-            dd.v[i] = (T)dstep;
-            par[i] = i < valid ? dp * ui : 0.f;
-            par[G::EPT + i] = i < valid ? dstep : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < G::EPT; ++i) {
+            du.v[i] = (T)fmaf(step[i], gb[i], sskip[lc + i] * dp[i]);
+            dd.v[i] = (T)dstep[i];
+            par[i] = i < valid ? dp[i] * (float)u.v[i] : 0.f;
+            par[G::EPT + i] = i < valid ? dstep[i] : 0.f;
         }
         if (a.grad.du.data) store_pack<T, G::EPT>(row_out<T>(a.grad.du, r) + d0 + lc, du, valid);
         if (a.grad.ddelta.data) store_pack<T, G::EPT>(row_out<T>(a.grad.ddelta, r) + d0 + lc, dd, valid);
