@@ -11,7 +11,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libaug.so")
 SOURCES = ["aug_api.hip", "pack_kernels.hip", "rir_kernels.hip", "conv_kernels.hip", "mel_kernels.hip", "vtlp_kernels.hip",
-           "rows_api.hip", "norm_kernels.hip", "short_conv_kernels.hip", "scan_kernels.hip"]
+           "rows_api.hip", "rows_kernels.hip", "norm_kernels.hip", "short_conv_kernels.hip", "scan_kernels.hip"]
 
 # Packed-FP32 instructions are switched off for every kernel; the image-sum file is
 # also built without FMA contraction because its tap index must follow a fixed fp64

@@ -74,43 +74,9 @@ __global__ __launch_bounds__(64) void norm_backward_kernel(NormBackArgs a) {
     }
 }
 
-// 64 columns to a group, every fourth row a wavefront's, eight rows' loads on their way at once (one row after another took 38 us for
-// 128 rows).
-constexpr int kColumns = 64;
-__global__ __launch_bounds__(4 * kColumns) void sum_partials_kernel(const float* partial, int n_partial, int64_t stride, SumOuts outs) {
-    __shared__ float part[4][kColumns];
-    const int lane = threadIdx.x % kColumns, wave = threadIdx.x / kColumns;
-    const int64_t c = (int64_t)blockIdx.x * kColumns + lane, width = outs.part[0].width + outs.part[1].width + outs.part[2].width;
-    constexpr int kAhead = 8;
-    float acc = 0.f;
-    for (int p = wave; p < n_partial; p += 4 * kAhead) {
-        float v[kAhead];
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) v[j] = c < width && p + 4 * j < n_partial ? partial[(p + 4 * j) * stride + c] : 0.f;
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) acc += v[j];
-    }
-    part[wave][lane] = acc;
-    __syncthreads();
-    if (wave || c >= width) return;
-    const float sum = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
-    int64_t at = c;
-    for (const SumOuts::Out& o : outs.part) {
-        if (at >= 0 && at < o.width && o.out) o.out[at] = sum;
-        at -= o.width;
-    }
-}
-
 int rows_per_partial(int64_t n_rows) { return (int)((n_rows + 1023) / 1024 < 64 ? 64 : (n_rows + 1023) / 1024); }
 
 }  // namespace
-
-hipError_t launch_sum_partials(hipStream_t s, const float* partial, int n_partial, int64_t stride, const SumOuts& outs) {
-    const int64_t width = outs.part[0].width + outs.part[1].width + outs.part[2].width;
-    if (width <= 0) return hipSuccess;
-    sum_partials_kernel<<<dim3((unsigned)((width + kColumns - 1) / kColumns)), dim3(4 * kColumns), 0, s>>>(partial, n_partial, stride, outs);
-    return hipGetLastError();
-}
 
 hipError_t launch_norm(hipStream_t s, const NormArgs& a, int) {
     return with_type(a.cfg.dtype, [&](auto t) {

@@ -14,6 +14,22 @@ struct RowBlocks {
     const int2* items = nullptr;         // device [n_items]: (sequence, block of it)
 };
 
+constexpr int kWholeLg = 30;             // blocks of whole sequences
+
+// The device's tables of a batch of sequences from what the host left in pinned memory: begin and end (null: they are there already)
+// and the exclusive prefix sum of the blocks, n_seq + 1 entries each.  With `whole`, a block per sequence, `first` gives instead the
+// place of each sequence in the table of blocks.
+struct RowTableArgs {
+    int n_seq;
+    bool whole;
+    const int64_t *begin, *end;
+    const int* first;
+    int64_t *d_begin, *d_end;
+    int* d_first;
+    int2* items;
+};
+hipError_t launch_row_tables(hipStream_t s, const RowTableArgs& a);
+
 // Sums of the columns of partial [n_partial][stride] into up to three arrays that follow one another in a row of it (null: not wanted).
 // The terms of a column are added in an order that depends on n_partial only.
 struct SumOuts {
@@ -78,7 +94,9 @@ struct ScanArgs {
     aug_scan_grad grad;
     void* ws;
 };
+// Rows of a block as a power of two, kWholeLg: sequences are not cut; of those, how many a row of work groups across the chip takes.
 int scan_lg_block(const aug_scan_cfg& cfg, int n_seq, const int64_t* begin, const int64_t* lengths, int n_cu, bool backward);
+int scan_abreast(const aug_scan_cfg& cfg, int n_cu);
 size_t scan_workspace(const aug_scan_cfg& cfg, int n_items, int64_t n_rows, int n_cu, bool backward);     // bytes
 hipError_t launch_scan(hipStream_t s, const ScanArgs& a, int n_cu);
 hipError_t launch_scan_backward(hipStream_t s, const ScanArgs& a, int64_t n_rows, int n_cu);

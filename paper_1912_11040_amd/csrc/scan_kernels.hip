@@ -47,7 +47,7 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, float* first_stat
     const int d0 = group * per_group + in_group, width = min(G::CW, per_group - in_group);
     const int2 item = a.rows.items[blockIdx.y];
     const int64_t seq = item.x, begin = a.rows.begin[seq] + ((int64_t)item.y << a.rows.lg), end = a.rows.end[seq];
-    const bool last = a.rows.lg == 30 || blockIdx.y + 1 == gridDim.y || a.rows.items[blockIdx.y + 1].y == 0;
+    const bool last = a.rows.lg == kWholeLg || blockIdx.y + 1 == gridDim.y || a.rows.items[blockIdx.y + 1].y == 0;
     if (MODE == kSums && last) return;                   // nobody asks for a sequence's last sums
     const int rows = (int)min(end - begin, (int64_t)1 << a.rows.lg);
 
@@ -753,7 +753,7 @@ int scan_lg_block(const aug_scan_cfg& cfg, int n_seq, const int64_t* begin, cons
         longest = longest > len ? longest : len;
     }
     const int64_t tiles = scan_tiles(cfg), filled = rows * tiles / n_cu;      // rows per compute unit
-    if (longest < 256 || (longest > filled ? longest : filled) < 2 * filled + 128) return 30;
+    if (longest < 256 || (longest > filled ? longest : filled) < 2 * filled + 128) return kWholeLg;
     int lg = 10;
     while (lg > 6 && (rows >> lg) * tiles < 4 * (int64_t)n_cu) --lg;
     return lg;
@@ -775,6 +775,10 @@ BackPlan back_plan(const aug_scan_cfg& cfg, int n_items, int n_cu) {
     p.runs = (int)(runs < n_items ? runs : n_items);
     return p;
 }
+int scan_abreast(const aug_scan_cfg& cfg, int n_cu) {
+    const int n = n_cu / scan_tiles(cfg);
+    return n < 1 ? 1 : n;
+}
 size_t scan_workspace(const aug_scan_cfg& cfg, int n_items, int64_t n_rows, int n_cu, bool backward) {
     if (!backward) return 4 * (size_t)n_items * cfg.dim * (cfg.n_state + 1);      // first states, steps' sums
     const BackPlan p = back_plan(cfg, n_items, n_cu);
@@ -788,7 +792,7 @@ hipError_t launch_scan(hipStream_t s, const ScanArgs& a, int) {
             const dim3 grid((unsigned)scan_tiles(a.cfg), (unsigned)a.rows.n_items);
             float* const first_state = static_cast<float*>(a.ws);
             float* const step_sum = first_state + (int64_t)a.rows.n_items * a.cfg.dim * a.cfg.n_state;
-            if (a.rows.lg == 30) {
+            if (a.rows.lg == kWholeLg) {
                 scan_kernel<T, ln.value, k.value, kWhole><<<grid, dim3(256), 0, s>>>(a, nullptr, nullptr);
                 return hipGetLastError();
             }
