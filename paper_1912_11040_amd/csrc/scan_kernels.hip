@@ -173,31 +173,76 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, float* first_stat
     }
 }
 
-// Turns each block's end state from zero (first_state as kSums leaves it) into its first state: a thread per (sequence, state) goes
-// through the sequence's blocks, h' = F + exp(a sum of steps) h, with eight blocks' loads on their way at once.
-__global__ __launch_bounds__(64) void scan_join_kernel(ScanArgs a, float* first_state, const float* step_sum) {
-    const int64_t width = (int64_t)a.cfg.dim * a.cfg.n_state, i = (int64_t)blockIdx.x * 64 + threadIdx.x;
-    if (i >= width) return;
-    const int seq = blockIdx.y, from = a.rows.first[seq], to = a.rows.first[seq + 1];
-    const int64_t d = i / a.cfg.n_state;
-    const float rate = rate2(a.in.a[i]);
-    float h = a.state_in ? a.state_in[seq * width + i] : 0.f;
-    constexpr int kAhead = 8;
-    for (int at = from; at < to; at += kAhead) {
-        float f[kAhead], s[kAhead];
+// Through the blocks of a sequence: values[j] becomes what comes into block j, h_0 = h, h_{j+1} = values[j] + exp(rate sum of j's steps) h_j,
+// for one of `width` states.  GROUPS groups of lanes take eight blocks each at a time, whose loads are on their way together: with
+// eight groups 64 blocks a round, where the states alone do not fill the chip (384 channels of 282 blocks: 10 us, with one group 35);
+// with one nothing is exchanged (32 sequences of 27 blocks, 16384 states, both ways: 50 us, the memory's rate; with eight 67).  Block j
+// lies at from + j dir; from block `known` on nothing is known or asked for.  All threads call it; states beyond the width are only
+// there for the barriers.
+constexpr int kJoinAhead = 8;
+template <int GROUPS> constexpr int kJoinStates = GROUPS == 1 ? 64 : 32;
+template <int GROUPS> struct JoinShared {
+    float value[GROUPS][kJoinStates<GROUPS>], steps[GROUPS][kJoinStates<GROUPS>];
+};
+bool join_in_groups(int64_t width, int n_seq, int n_items, int n_cu) {
+    return n_items / n_seq > 16 && width * n_seq < 64 * 8 * (int64_t)n_cu;       // fewer than eight wavefronts to a compute unit
+}
+__device__ inline float pass_block(float h, float value, float steps, float rate) {
+    // (a state of zero stays out of it, also where a rate above zero makes the factor infinite)
+    return h == 0.f ? value : fmaf(__builtin_amdgcn_exp2f(steps * rate), h, value);
+}
+template <int GROUPS>
+__device__ inline void join_blocks(JoinShared<GROUPS>& sh, float* values, const float* steps, int64_t width, int64_t i, int dim, int64_t d, float rate, float h,
+                                   int from, int dir, int n, int known) {
+    const int lane = threadIdx.x % kJoinStates<GROUPS>, group = threadIdx.x / kJoinStates<GROUPS>;
+    for (int base = 0; base < n; base += GROUPS * kJoinAhead) {
+        const int j0 = base + group * kJoinAhead;
+        float f[kJoinAhead], s[kJoinAhead];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const bool there = at + j < to - 1;          // the last block's end is not asked for
-            f[j] = there ? first_state[(at + j) * width + i] : 0.f;
-            s[j] = there ? step_sum[(int64_t)(at + j) * a.cfg.dim + d] : 0.f;
+        for (int q = 0; q < kJoinAhead; ++q) {
+            const bool there = i < width && j0 + q < known;
+            const int64_t at = from + (int64_t)(j0 + q) * dir;
+            f[q] = there ? values[at * width + i] : 0.f;
+            s[q] = there ? steps[at * dim + d] : 0.f;
+        }
+        float in = h;
+        if constexpr (GROUPS > 1) {
+            float value = 0.f, sum = 0.f;
+#pragma unroll
+            for (int q = 0; q < kJoinAhead; ++q) {
+                value = pass_block(value, f[q], s[q], rate);
+                sum += s[q];
+            }
+            sh.value[group][lane] = value;
+            sh.steps[group][lane] = sum;
+            __syncthreads();
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                if (g == group) in = h;
+                h = pass_block(h, sh.value[g][lane], sh.steps[g][lane], rate);
+            }
         }
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            if (at + j < to) first_state[(at + j) * width + i] = h;
-            // (a state of zero stays out of it, also where a rate above zero makes the factor infinite)
-            h = h == 0.f ? f[j] : fmaf(__builtin_amdgcn_exp2f(s[j] * rate), h, f[j]);
+        for (int q = 0; q < kJoinAhead; ++q) {
+            if (i < width && j0 + q < n) values[(from + (int64_t)(j0 + q) * dir) * width + i] = in;
+            in = pass_block(in, f[q], s[q], rate);
+        }
+        if constexpr (GROUPS > 1) {
+            __syncthreads();
+        } else {
+            h = in;
         }
     }
+}
+
+// Turns each block's end state from zero (first_state as kSums leaves it; the last block's is not known) into its first state.
+template <int GROUPS> __global__ __launch_bounds__(kJoinStates<GROUPS> * GROUPS) void scan_join_kernel(ScanArgs a, float* first_state, const float* step_sum) {
+    __shared__ JoinShared<GROUPS> sh;
+    const int64_t width = (int64_t)a.cfg.dim * a.cfg.n_state, i = (int64_t)blockIdx.x * kJoinStates<GROUPS> + threadIdx.x % kJoinStates<GROUPS>;
+    const int seq = blockIdx.y, from = a.rows.first[seq], n = a.rows.first[seq + 1] - from;
+    const int64_t d = i / a.cfg.n_state;
+    const float rate = i < width ? rate2(a.in.a[i]) : 0.f, h = a.state_in && i < width ? a.state_in[seq * width + i] : 0.f;
+    join_blocks(sh, first_state, step_sum, width, i, a.cfg.dim, d, rate, h, from, 1, n, n - 1);
 }
 
 // ---- rows of streams ----
@@ -372,42 +417,16 @@ __global__ __launch_bounds__(256) void scan_back_sums_kernel(ScanArgs a, BackWs 
     if (tid % LN == 0) ws.steps[(int64_t)blockIdx.y * dim + d0 + ch] = sum;
 }
 
-// A thread per (sequence, state): forward through the blocks for their first states, back for what comes in from behind.
-__global__ __launch_bounds__(64) void scan_back_join_kernel(ScanArgs a, BackWs ws) {
-    const int64_t width = (int64_t)a.cfg.dim * a.cfg.n_state, i = (int64_t)blockIdx.x * 64 + threadIdx.x;
-    const int seq = blockIdx.y, from = a.rows.first[seq], to = a.rows.first[seq + 1];
-    if (i >= width || a.rows.end[seq] == a.rows.begin[seq]) return;
+// Forward through a sequence's blocks for their first states, back for what comes in from behind.
+template <int GROUPS> __global__ __launch_bounds__(kJoinStates<GROUPS> * GROUPS) void scan_back_join_kernel(ScanArgs a, BackWs ws) {
+    __shared__ JoinShared<GROUPS> sh;
+    const int64_t width = (int64_t)a.cfg.dim * a.cfg.n_state, i = (int64_t)blockIdx.x * kJoinStates<GROUPS> + threadIdx.x % kJoinStates<GROUPS>;
+    const int seq = blockIdx.y, from = a.rows.first[seq], n = a.rows.first[seq + 1] - from;
+    if (a.rows.end[seq] == a.rows.begin[seq]) return;    // (an empty sequence's block has no sums)
     const int64_t d = i / a.cfg.n_state;
-    const float rate = rate2(a.in.a[i]);
-    constexpr int kAhead = 8;
-    float h = a.state_in ? a.state_in[seq * width + i] : 0.f;
-    for (int at = from; at < to; at += kAhead) {
-        float f[kAhead], s[kAhead];
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            f[j] = at + j < to ? ws.first[(at + j) * width + i] : 0.f;
-            s[j] = at + j < to ? ws.steps[(int64_t)(at + j) * a.cfg.dim + d] : 0.f;
-        }
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            if (at + j < to) ws.first[(at + j) * width + i] = h;
-            h = h == 0.f ? f[j] : fmaf(__builtin_amdgcn_exp2f(s[j] * rate), h, f[j]);
-        }
-    }
-    float g = 0.f;
-    for (int at = to - 1; at >= from; at -= kAhead) {
-        float f[kAhead], s[kAhead];
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            f[j] = at - j >= from ? ws.behind[(at - j) * width + i] : 0.f;
-            s[j] = at - j >= from ? ws.steps[(int64_t)(at - j) * a.cfg.dim + d] : 0.f;
-        }
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            if (at - j >= from) ws.behind[(at - j) * width + i] = g;
-            g = g == 0.f ? f[j] : fmaf(__builtin_amdgcn_exp2f(s[j] * rate), g, f[j]);
-        }
-    }
+    const float rate = i < width ? rate2(a.in.a[i]) : 0.f, h = a.state_in && i < width ? a.state_in[seq * width + i] : 0.f;
+    join_blocks(sh, ws.first, ws.steps, width, i, a.cfg.dim, d, rate, h, from, 1, n, n);
+    join_blocks(sh, ws.behind, ws.steps, width, i, a.cfg.dim, d, rate, 0.f, from + n - 1, -1, n, n);
 }
 
 // What a walker reads of a row: its channel's step, step u and dp, its states' b or c.  Rows are read one ahead of their use: the
@@ -718,7 +737,14 @@ __global__ __launch_bounds__(256) void scan_bc_kernel(ScanArgs a, BackWs ws, Bac
         const int64_t r = begin + i / width;
         const int group = (i % width) / (2 * n_state), k = (i % width) % (2 * n_state);
         float acc = 0.f;
-        for (int t = 0; t < tiles; ++t) acc += ws.bc[((int64_t)(group * tiles + t) * n_rows + r) * 2 * n_state + k];
+        constexpr int kAhead = 8;                        // tiles whose sums are on their way together
+        for (int t = 0; t < tiles; t += kAhead) {
+            float v[kAhead];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) v[j] = t + j < tiles ? ws.bc[((int64_t)(group * tiles + t + j) * n_rows + r) * 2 * n_state + k] : 0.f;
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) acc += v[j];
+        }
         const aug_rows& out = k < n_state ? a.grad.db : a.grad.dc;
         if (out.data) row_out<T>(out, r)[group * n_state + (k < n_state ? k : k - n_state)] = (T)acc;
     }
@@ -758,6 +784,11 @@ int scan_lg_block(const aug_scan_cfg& cfg, int n_seq, const int64_t* begin, cons
     while (lg > 6 && (rows >> lg) * tiles < 4 * (int64_t)n_cu) --lg;
     return lg;
 }
+template <class F> void with_groups(bool eight, F f) {
+    if (eight) f(std::integral_constant<int, 8>());
+    else f(std::integral_constant<int, 1>());
+}
+
 // The gradients' lanes: at least four per channel, so that a block's elements are eight to a lane at most.
 template <class F> hipError_t with_back_lanes(int n_state, F f) {
     using std::integral_constant;
@@ -785,7 +816,7 @@ size_t scan_workspace(const aug_scan_cfg& cfg, int n_items, int64_t n_rows, int 
     return 4 * ((size_t)n_items * cfg.dim * (2 * cfg.n_state + 1) + (size_t)p.tiles * n_rows * 2 * cfg.n_state + (size_t)p.runs * cfg.dim * (cfg.n_state + 2));
 }
 
-hipError_t launch_scan(hipStream_t s, const ScanArgs& a, int) {
+hipError_t launch_scan(hipStream_t s, const ScanArgs& a, int n_cu) {
     return with_type(a.cfg.dtype, [&](auto t) {
         return with_lanes(a.cfg.n_state, [&](auto ln, auto k) {
             using T = decltype(t);
@@ -800,7 +831,10 @@ hipError_t launch_scan(hipStream_t s, const ScanArgs& a, int) {
             hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
             const int64_t width = (int64_t)a.cfg.dim * a.cfg.n_state;
-            scan_join_kernel<<<dim3((unsigned)((width + 63) / 64), (unsigned)a.rows.n_seq), dim3(64), 0, s>>>(a, first_state, step_sum);
+            with_groups(join_in_groups(width, a.rows.n_seq, a.rows.n_items, n_cu), [&](auto g) {
+                constexpr int n = kJoinStates<g.value>;
+                scan_join_kernel<g.value><<<dim3((unsigned)((width + n - 1) / n), (unsigned)a.rows.n_seq), dim3(n * g.value), 0, s>>>(a, first_state, step_sum);
+            });
             e = hipGetLastError();
             if (e != hipSuccess) return e;
             scan_kernel<T, ln.value, k.value, kResume><<<grid, dim3(256), 0, s>>>(a, first_state, step_sum);
@@ -835,7 +869,10 @@ hipError_t launch_scan_backward(hipStream_t s, const ScanArgs& a, int64_t n_rows
                 scan_back_sums_kernel<T, ln.value, k.value><<<dim3((unsigned)plan.tiles, (unsigned)a.rows.n_items), dim3(256), 0, s>>>(a, ws);
                 hipError_t e = hipGetLastError();
                 if (e != hipSuccess) return e;
-                scan_back_join_kernel<<<dim3((unsigned)((width + 63) / 64), (unsigned)a.rows.n_seq), dim3(64), 0, s>>>(a, ws);
+                with_groups(join_in_groups(width, a.rows.n_seq, a.rows.n_items, n_cu), [&](auto g) {
+                constexpr int n = kJoinStates<g.value>;
+                scan_back_join_kernel<g.value><<<dim3((unsigned)((width + n - 1) / n), (unsigned)a.rows.n_seq), dim3(n * g.value), 0, s>>>(a, ws);
+            });
                 e = hipGetLastError();
                 if (e != hipSuccess) return e;
             }
