@@ -1,105 +1,247 @@
 // Root-mean-square norm of rows with the residual's addition and an 8-bit output, and its gradients.
+//
+// Both are bound by memory.  A row belongs to TPR lanes, each with NV stretches of eight columns in registers from the first read
+// to the last write, so that every matrix goes over the bus once; lanes go from row to row with their columns' weights (and
+// the weights' gradients) in registers.
+
+#include <type_traits>
 
 #include "rows_device.h"
 
 namespace aug {
 namespace {
 
-// One wavefront per row: the sum of squares, then block by block the largest magnitude and the outputs.
-template <class T>
-__global__ __launch_bounds__(64) void norm_kernel(NormArgs a) {
-    const int lane = threadIdx.x, dim = a.cfg.dim;
-    const int64_t r = blockIdx.x;
-    const T* x = row_in<T>(a.x, r);
-    const T* res = a.residual.data ? row_in<T>(a.residual, r) : nullptr;
-    float ss = 0.f;
-    for (int d = lane; d < dim; d += 64) {
-        const float s = (float)x[d] + (res ? (float)res[d] : 0.f);
-        ss += s * s;
+constexpr int kThreads = 256, kVec = 8;
+
+// The sum over a row's lanes, in all of them.
+template <int TPR> __device__ inline float row_sum(float v, float* exchange) {
+    v = lanes_sum<(TPR < 64 ? TPR : 64)>(v);
+    if constexpr (TPR == kThreads) {
+        __syncthreads();                                 // (the last row's sums have been read)
+        if (threadIdx.x % 64 == 0) exchange[threadIdx.x / 64] = v;
+        __syncthreads();
+        v = (exchange[0] + exchange[1]) + (exchange[2] + exchange[3]);
     }
-    const float rstd = 1.f / sqrtf(wave_sum(ss) / (float)dim + a.cfg.eps);
-    if (a.rstd && lane == 0) a.rstd[r] = rstd;
-    const int width = a.cfg.q_block ? a.cfg.q_block : dim, n_blocks = (dim + width - 1) / width;
-    for (int b = 0; b < n_blocks; ++b) {
-        const int from = b * width, to = min(from + width, dim);
-        float scale = 0.f;
-        if (a.q.data) {
-            unsigned most = 0;
-            for (int d = from + lane; d < to; d += 64) {
-                const float s = (float)x[d] + (res ? (float)res[d] : 0.f);
-                const unsigned m = __float_as_uint(s * rstd * (a.weight ? a.weight[d] : 1.f)) & 0x7fffffffu;
-                most = most > m ? most : m;
-            }
-            scale = __uint_as_float(wave_max(most)) / 448.f;
-            if (lane == 0) a.scale[r * n_blocks + b] = scale;
+    return v;
+}
+
+template <class T, int TPR, int NV>
+__global__ __launch_bounds__(kThreads) void norm_kernel(NormArgs a) {
+    __shared__ float exchange[8];
+    const int lane = threadIdx.x % TPR, dim = a.cfg.dim;
+    const int64_t step = (int64_t)gridDim.x * (kThreads / TPR);
+    const int width = a.cfg.q_block && a.cfg.q_block < kVec * TPR ? a.cfg.q_block : dim;      // columns of a block; no block ends inside a lane's eight
+    const bool whole = width >= dim;
+    const int n_blocks = a.cfg.q_block ? (dim + a.cfg.q_block - 1) / a.cfg.q_block : 1;
+    float w[NV][kVec];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int c = (j * TPR + lane) * kVec;
+        const Pack<float, kVec> v = a.weight ? load_pack<float, kVec>(a.weight + c, dim - c) : Pack<float, kVec>{1, 1, 1, 1, 1, 1, 1, 1};
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) w[j][i] = v.v[i];
+    }
+    for (int64_t r = (int64_t)blockIdx.x * (kThreads / TPR) + threadIdx.x / TPR; r < a.n_rows; r += step) {
+        float s[NV][kVec];
+        Pack<T, kVec> x[NV], res[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c = (j * TPR + lane) * kVec;
+            x[j] = load_pack<T, kVec>(row_in<T>(a.x, r) + c, dim - c);
+            if (a.residual.data) res[j] = load_pack<T, kVec>(row_in<T>(a.residual, r) + c, dim - c);
         }
-        for (int d = from + lane; d < to; d += 64) {
-            const float s = (float)x[d] + (res ? (float)res[d] : 0.f);
-            const float y = s * rstd * (a.weight ? a.weight[d] : 1.f);
-            if (a.sum.data) row_out<T>(a.sum, r)[d] = (T)s;
-            if (a.y.data) row_out<T>(a.y, r)[d] = (T)y;
-            if (a.q.data) {
-                const float v = scale == 0.f ? 0.f : y / scale;
-                row_out<uint8_t>(a.q, r)[d] = (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(v, v, 0, false) & 0xff);
+        float ss = 0.f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c = (j * TPR + lane) * kVec;
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) s[j][i] = (float)x[j].v[i] + (a.residual.data ? (float)res[j].v[i] : 0.f);
+            float part = 0.f;                            // (the squares of a stretch by themselves: shorter sums)
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) part = fmaf(s[j][i], s[j][i], part);
+            ss += part;
+            if (a.sum.data) {
+                Pack<T, kVec> out;
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) out.v[i] = (T)s[j][i];
+                store_pack<T, kVec>(row_out<T>(a.sum, r) + c, out, dim - c);
             }
+        }
+        const float rstd = 1.f / sqrtf(row_sum<TPR>(ss, exchange) / (float)dim + a.cfg.eps);
+        if (a.rstd && lane == 0) a.rstd[r] = rstd;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c = (j * TPR + lane) * kVec;
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) s[j][i] *= rstd * w[j][i];
+            if (a.y.data) {
+                Pack<T, kVec> out;
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) out.v[i] = (T)s[j][i];
+                store_pack<T, kVec>(row_out<T>(a.y, r) + c, out, dim - c);
+            }
+        }
+        if (!a.q.data) continue;
+        // the largest magnitude by its bits: a NaN's are larger than any number's
+        unsigned most[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            most[j] = 0;
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                const unsigned m = __float_as_uint(s[j][i]) & 0x7fffffffu;
+                most[j] = most[j] > m ? most[j] : m;
+            }
+        }
+        if (whole) {
+#pragma unroll
+            for (int j = 1; j < NV; ++j) most[0] = most[0] > most[j] ? most[0] : most[j];
+            most[0] = lanes_max(most[0], TPR < 64 ? TPR : 64);
+            if constexpr (TPR == kThreads) {
+                __syncthreads();
+                if (threadIdx.x % 64 == 0) exchange[4 + threadIdx.x / 64] = __uint_as_float(most[0]);
+                __syncthreads();
+                for (int i = 0; i < 4; ++i) most[0] = max(most[0], __float_as_uint(exchange[4 + i]));
+            }
+#pragma unroll
+            for (int j = 1; j < NV; ++j) most[j] = most[0];
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c = (j * TPR + lane) * kVec;
+            if (!whole) most[j] = lanes_max(most[j], width / kVec);
+            const float scale = __uint_as_float(most[j]) / 448.f;
+            if (c < dim && (whole ? c == 0 : c % width == 0)) a.scale[r * n_blocks + (whole ? 0 : c / width)] = scale;
+            const float by = scale == 0.f ? 1.f : scale;
+            Pack<unsigned, 2> out;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                unsigned v = __builtin_amdgcn_cvt_pk_fp8_f32(s[j][4 * i] / by, s[j][4 * i + 1] / by, 0, false);
+                out.v[i] = __builtin_amdgcn_cvt_pk_fp8_f32(s[j][4 * i + 2] / by, s[j][4 * i + 3] / by, v, true);
+            }
+            Pack<uint8_t, kVec> bytes;
+            __builtin_memcpy(bytes.v, out.v, kVec);
+            store_pack<uint8_t, kVec>(row_out<uint8_t>(a.q, r) + c, bytes, dim - c);
         }
     }
 }
 
-// dweight's part of 64 rows, a thread per column.
-template <class T>
-__global__ __launch_bounds__(64) void norm_dweight_kernel(NormBackArgs a, int rows) {
-    const int d = blockIdx.x * 64 + threadIdx.x;
-    if (d >= a.dim) return;
-    float acc = 0.f;
-    const int64_t from = (int64_t)blockIdx.y * rows, to = min(from + rows, a.n_rows);
-    for (int64_t r = from; r < to; ++r) acc += (float)row_in<T>(a.dy, r)[d] * ((float)row_in<T>(a.sum, r)[d] * a.rstd[r]);
-    a.partial[(int64_t)blockIdx.y * a.dim + d] = acc;
-}
-
-template <class T>
-__global__ __launch_bounds__(64) void norm_backward_kernel(NormBackArgs a) {
-    const int lane = threadIdx.x;
-    const int64_t r = blockIdx.x;
-    const T* x = row_in<T>(a.sum, r);
-    const T* dy = row_in<T>(a.dy, r);
-    const float rstd = a.rstd[r];
-    float dot = 0.f;
-    for (int d = lane; d < a.dim; d += 64) dot += (float)x[d] * ((float)dy[d] * (a.weight ? a.weight[d] : 1.f));
-    const float slope = wave_sum(dot) / (float)a.dim * rstd * rstd * rstd;
-    for (int d = lane; d < a.dim; d += 64) {
-        float g = (float)dy[d] * (a.weight ? a.weight[d] : 1.f) * rstd - (float)x[d] * slope;
-        if (a.dsum.data) g += (float)row_in<T>(a.dsum, r)[d];
-        row_out<T>(a.dx, r)[d] = (T)g;
+template <class T, int TPR, int NV>
+__global__ __launch_bounds__(kThreads) void norm_backward_kernel(NormBackArgs a) {
+    constexpr int kGroups = kThreads / TPR;
+    __shared__ float exchange[4];
+    __shared__ float sums[TPR == kThreads ? 1 : kGroups][TPR == kThreads ? 1 : TPR * NV * kVec];
+    const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR, dim = a.dim;
+    float w[NV][kVec], dw[NV][kVec] = {};
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int c = (j * TPR + lane) * kVec;
+        const Pack<float, kVec> v = a.weight ? load_pack<float, kVec>(a.weight + c, dim - c) : Pack<float, kVec>{1, 1, 1, 1, 1, 1, 1, 1};
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) w[j][i] = v.v[i];
+    }
+    for (int64_t r = (int64_t)blockIdx.x * kGroups + group; r < a.n_rows; r += (int64_t)gridDim.x * kGroups) {
+        const float rstd = a.rstd[r];
+        Pack<T, kVec> x[NV], dy[NV], ds[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c = (j * TPR + lane) * kVec;
+            x[j] = load_pack<T, kVec>(row_in<T>(a.sum, r) + c, dim - c);
+            dy[j] = load_pack<T, kVec>(row_in<T>(a.dy, r) + c, dim - c);
+            if (a.dsum.data) ds[j] = load_pack<T, kVec>(row_in<T>(a.dsum, r) + c, dim - c);
+        }
+        float dot = 0.f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            float part = 0.f;
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                const float xi = (float)x[j].v[i], g = (float)dy[j].v[i];
+                part = fmaf(xi, g * w[j][i], part);
+                dw[j][i] = fmaf(g, xi * rstd, dw[j][i]);
+            }
+            dot += part;
+        }
+        if (!a.dx.data) continue;
+        const float slope = row_sum<TPR>(dot, exchange) / (float)dim * rstd * rstd * rstd;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c = (j * TPR + lane) * kVec;
+            Pack<T, kVec> out;
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) {
+                float g = fmaf((float)dy[j].v[i] * w[j][i], rstd, -(float)x[j].v[i] * slope);
+                if (a.dsum.data) g += (float)ds[j].v[i];
+                out.v[i] = (T)g;
+            }
+            store_pack<T, kVec>(row_out<T>(a.dx, r) + c, out, dim - c);
+        }
+    }
+    if (!a.partial) return;
+    float* const out = a.partial + (int64_t)blockIdx.x * dim;
+    if constexpr (TPR == kThreads) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < kVec; ++i)
+                if ((j * TPR + lane) * kVec + i < dim) out[(j * TPR + lane) * kVec + i] = dw[j][i];
+    } else {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) sums[group][(j * TPR + lane) * kVec + i] = dw[j][i];
+        __syncthreads();
+        for (int c = threadIdx.x; c < dim; c += kThreads) {
+            float sum = 0.f;
+            for (int g = 0; g < kGroups; ++g) sum += sums[g][c];
+            out[c] = sum;
+        }
     }
 }
 
-int rows_per_partial(int64_t n_rows) { return (int)((n_rows + 1023) / 1024 < 64 ? 64 : (n_rows + 1023) / 1024); }
+// Calls f with the lanes per row and the stretches per lane for rows of so many columns: the fewest lanes, so that a wavefront has much
+// to ask for at once, as far as a lane's columns and weights fit its registers.
+template <class F> hipError_t with_row(int dim, F f) {
+    using std::integral_constant;
+    if (dim <= 128) return f(integral_constant<int, 16>(), integral_constant<int, 1>());
+    if (dim <= 512) return f(integral_constant<int, 64>(), integral_constant<int, 1>());
+    if (dim <= 1024) return f(integral_constant<int, 64>(), integral_constant<int, 2>());
+    if (dim <= 2048) return f(integral_constant<int, 64>(), integral_constant<int, 4>());
+    if (dim <= 4096) return f(integral_constant<int, 256>(), integral_constant<int, 2>());
+    if (dim <= 8192) return f(integral_constant<int, 256>(), integral_constant<int, 4>());
+    return f(integral_constant<int, 256>(), integral_constant<int, 8>());
+}
+// Work groups that go through the rows together: as many as there are rows for, `most` per compute unit.
+int norm_groups(int64_t n_rows, int dim, int n_cu, int most) {
+    const int per_group = kThreads / (dim <= 128 ? 16 : dim <= 2048 ? 64 : 256);
+    const int64_t groups = (n_rows + per_group - 1) / per_group;
+    return (int)(groups < (int64_t)most * n_cu ? groups : (int64_t)most * n_cu);
+}
+constexpr int kForwardGroups = 8, kBackwardGroups = 4;
 
 }  // namespace
 
-hipError_t launch_norm(hipStream_t s, const NormArgs& a, int) {
+hipError_t launch_norm(hipStream_t s, const NormArgs& a, int n_cu) {
     return with_type(a.cfg.dtype, [&](auto t) {
-        norm_kernel<decltype(t)><<<dim3((unsigned)a.n_rows), dim3(64), 0, s>>>(a);
-        return hipGetLastError();
+        return with_row(a.cfg.dim, [&](auto tpr, auto nv) {
+            norm_kernel<decltype(t), tpr.value, nv.value><<<dim3((unsigned)norm_groups(a.n_rows, a.cfg.dim, n_cu, kForwardGroups)), dim3(kThreads), 0, s>>>(a);
+            return hipGetLastError();
+        });
     });
 }
 
-int norm_partials(int64_t n_rows, int, int) { return (int)((n_rows + rows_per_partial(n_rows) - 1) / rows_per_partial(n_rows)); }
+int norm_partials(int64_t n_rows, int dim, int n_cu) { return norm_groups(n_rows, dim, n_cu, kBackwardGroups); }
 
 hipError_t launch_norm_backward(hipStream_t s, const NormBackArgs& a, int n_cu) {
-    return with_type(a.dtype, [&](auto t) {
-        if (a.dweight) {                 // first: dx may take dy's place
-            const int n = norm_partials(a.n_rows, a.dim, n_cu);
-            norm_dweight_kernel<decltype(t)><<<dim3((unsigned)((a.dim + 63) / 64), (unsigned)n), dim3(64), 0, s>>>(a, rows_per_partial(a.n_rows));
-            hipError_t e = hipGetLastError();
-            if (e != hipSuccess) return e;
-            e = launch_sum_partials(s, a.partial, n, a.dim, {{{a.dweight, a.dim}, {}, {}}});
-            if (e != hipSuccess) return e;
-        }
-        if (a.dx.data) norm_backward_kernel<decltype(t)><<<dim3((unsigned)a.n_rows), dim3(64), 0, s>>>(a);
-        return hipGetLastError();
+    const int groups = norm_partials(a.n_rows, a.dim, n_cu);
+    hipError_t e = with_type(a.dtype, [&](auto t) {
+        return with_row(a.dim, [&](auto tpr, auto nv) {
+            norm_backward_kernel<decltype(t), tpr.value, nv.value><<<dim3((unsigned)groups), dim3(kThreads), 0, s>>>(a);
+            return hipGetLastError();
+        });
     });
+    if (e == hipSuccess && a.dweight) e = launch_sum_partials(s, a.partial, groups, a.dim, {{{a.dweight, a.dim}, {}, {}}});
+    return e;
 }
 
 }  // namespace aug

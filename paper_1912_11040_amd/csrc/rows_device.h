@@ -38,7 +38,7 @@ template <class T, int N> __device__ inline void store_pack(T* p, const Pack<T, 
         if (i < valid) p[i] = r.v[i];
 }
 
-// The sum over LN (a power of two up to 16) neighbouring lanes, in all of them: quads by permutation, then mirrored halves, whose
+// The sum over LN (a power of two) neighbouring lanes, in all of them: quads by permutation, then mirrored halves and swapped rows, whose
 // lanes hold equal sums already.
 template <int CTRL> __device__ inline float dpp_add(float v) {
     return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
@@ -48,6 +48,34 @@ template <int LN> __device__ inline float lanes_sum(float v) {
     if constexpr (LN >= 4) v = dpp_add<0x4E>(v);
     if constexpr (LN >= 8) v = dpp_add<0x141>(v);
     if constexpr (LN >= 16) v = dpp_add<0x140>(v);
+    if constexpr (LN >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if constexpr (LN >= 64) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    return v;
+}
+// The largest of so many neighbouring lanes' values likewise; `lanes` is the same for the whole wavefront.
+template <int CTRL> __device__ inline unsigned dpp_max(unsigned v) {
+    const unsigned o = __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true);
+    return v > o ? v : o;
+}
+__device__ inline unsigned lanes_max(unsigned v, int lanes) {
+    if (lanes >= 2) v = dpp_max<0xB1>(v);
+    if (lanes >= 4) v = dpp_max<0x4E>(v);
+    if (lanes >= 8) v = dpp_max<0x141>(v);
+    if (lanes >= 16) v = dpp_max<0x140>(v);
+    if (lanes >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        v = r[0] > r[1] ? r[0] : r[1];
+    }
+    if (lanes >= 64) {
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        v = r[0] > r[1] ? r[0] : r[1];
+    }
     return v;
 }
 
@@ -62,19 +90,6 @@ __device__ inline float softplus(float x) {
     const float e = exp_fast(-fabsf(x)), w = 1.f + e, d = w - 1.f;
     const float l = d == 0.f ? e : __builtin_amdgcn_logf(w) * 0.693147180559945309f * (e * __builtin_amdgcn_rcpf(d));
     return fmaxf(x, 0.f) + l;      // (a NaN is in l, whatever fmaxf drops)
-}
-
-__device__ inline float wave_sum(float v) {
-    for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
-    return v;
-}
-// The larger of two magnitudes' bits: a NaN's are larger than any number's.
-__device__ inline unsigned wave_max(unsigned v) {
-    for (int m = 32; m; m >>= 1) {
-        const unsigned o = __shfl_xor(v, m);
-        v = v > o ? v : o;
-    }
-    return v;
 }
 
 }  // namespace aug
