@@ -11,25 +11,28 @@
 namespace aug {
 namespace {
 
-constexpr int kThreads = 256, kVec = 8;
+constexpr int kVec = 8;
+template <int TPR> constexpr int kThreads = TPR < 256 ? 256 : TPR;      // a group's
 
 // The sum over a row's lanes, in all of them.
 template <int TPR> __device__ inline float row_sum(float v, float* exchange) {
     v = lanes_sum<(TPR < 64 ? TPR : 64)>(v);
-    if constexpr (TPR == kThreads) {
+    if constexpr (TPR > 64) {
         __syncthreads();                                 // (the last row's sums have been read)
         if (threadIdx.x % 64 == 0) exchange[threadIdx.x / 64] = v;
         __syncthreads();
-        v = (exchange[0] + exchange[1]) + (exchange[2] + exchange[3]);
+        v = exchange[0];
+#pragma unroll
+        for (int i = 1; i < TPR / 64; ++i) v += exchange[i];
     }
     return v;
 }
 
 template <class T, int TPR, int NV>
-__global__ __launch_bounds__(kThreads) void norm_kernel(NormArgs a) {
-    __shared__ float exchange[8];
+__global__ __launch_bounds__(kThreads<TPR>) void norm_kernel(NormArgs a) {
+    __shared__ float exchange[32];
     const int lane = threadIdx.x % TPR, dim = a.cfg.dim;
-    const int64_t step = (int64_t)gridDim.x * (kThreads / TPR);
+    const int64_t step = (int64_t)gridDim.x * (kThreads<TPR> / TPR);
     const int width = a.cfg.q_block && a.cfg.q_block < kVec * TPR ? a.cfg.q_block : dim;      // columns of a block; no block ends inside a lane's eight
     const bool whole = width >= dim;
     const int n_blocks = a.cfg.q_block ? (dim + a.cfg.q_block - 1) / a.cfg.q_block : 1;
@@ -41,7 +44,7 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(NormArgs a) {
 #pragma unroll
         for (int i = 0; i < kVec; ++i) w[j][i] = v.v[i];
     }
-    for (int64_t r = (int64_t)blockIdx.x * (kThreads / TPR) + threadIdx.x / TPR; r < a.n_rows; r += step) {
+    for (int64_t r = (int64_t)blockIdx.x * (kThreads<TPR> / TPR) + threadIdx.x / TPR; r < a.n_rows; r += step) {
         float s[NV][kVec];
         Pack<T, kVec> x[NV], res[NV];
 #pragma unroll
@@ -97,11 +100,11 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(NormArgs a) {
 #pragma unroll
             for (int j = 1; j < NV; ++j) most[0] = most[0] > most[j] ? most[0] : most[j];
             most[0] = lanes_max(most[0], TPR < 64 ? TPR : 64);
-            if constexpr (TPR == kThreads) {
+            if constexpr (TPR > 64) {
                 __syncthreads();
-                if (threadIdx.x % 64 == 0) exchange[4 + threadIdx.x / 64] = __uint_as_float(most[0]);
+                if (threadIdx.x % 64 == 0) exchange[16 + threadIdx.x / 64] = __uint_as_float(most[0]);
                 __syncthreads();
-                for (int i = 0; i < 4; ++i) most[0] = max(most[0], __float_as_uint(exchange[4 + i]));
+                for (int i = 0; i < TPR / 64; ++i) most[0] = max(most[0], __float_as_uint(exchange[16 + i]));
             }
 #pragma unroll
             for (int j = 1; j < NV; ++j) most[j] = most[0];
@@ -127,10 +130,10 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(NormArgs a) {
 }
 
 template <class T, int TPR, int NV>
-__global__ __launch_bounds__(kThreads) void norm_backward_kernel(NormBackArgs a) {
-    constexpr int kGroups = kThreads / TPR;
-    __shared__ float exchange[4];
-    __shared__ float sums[TPR == kThreads ? 1 : kGroups][TPR == kThreads ? 1 : TPR * NV * kVec];
+__global__ __launch_bounds__(kThreads<TPR>) void norm_backward_kernel(NormBackArgs a) {
+    constexpr int kGroups = kThreads<TPR> / TPR;
+    __shared__ float exchange[16];
+    __shared__ float sums[TPR >= 256 ? 1 : kGroups][TPR >= 256 ? 1 : TPR * NV * kVec];
     const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR, dim = a.dim;
     float w[NV][kVec], dw[NV][kVec] = {};
 #pragma unroll
@@ -179,7 +182,7 @@ __global__ __launch_bounds__(kThreads) void norm_backward_kernel(NormBackArgs a)
     }
     if (!a.partial) return;
     float* const out = a.partial + (int64_t)blockIdx.x * dim;
-    if constexpr (TPR == kThreads) {
+    if constexpr (TPR >= 256) {
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
@@ -191,7 +194,7 @@ __global__ __launch_bounds__(kThreads) void norm_backward_kernel(NormBackArgs a)
 #pragma unroll
             for (int i = 0; i < kVec; ++i) sums[group][(j * TPR + lane) * kVec + i] = dw[j][i];
         __syncthreads();
-        for (int c = threadIdx.x; c < dim; c += kThreads) {
+        for (int c = threadIdx.x; c < dim; c += kThreads<TPR>) {
             float sum = 0.f;
             for (int g = 0; g < kGroups; ++g) sum += sums[g][c];
             out[c] = sum;
@@ -199,44 +202,58 @@ __global__ __launch_bounds__(kThreads) void norm_backward_kernel(NormBackArgs a)
     }
 }
 
-// Calls f with the lanes per row and the stretches per lane for rows of so many columns: the fewest lanes, so that a wavefront has much
-// to ask for at once, as far as a lane's columns and weights fit its registers.
-template <class F> hipError_t with_row(int dim, F f) {
+// How a row of so many columns is dealt out: lanes per row, stretches per lane, and how many work groups go through the rows together per
+// compute unit.
+struct RowShape {
+    int lanes, vecs, groups;
+};
+// Forward: a row's whole width to a group where it takes one, so that many wavefronts have loads on their way (64 utterances at 2048
+// columns 183 us with a wavefront per row; 32 groups a compute unit 153, 16 162, 8 as many as 183: the last round is half empty).
+constexpr RowShape forward_shape(int dim) {
+    return dim <= 128 ? RowShape{16, 1, 16} : dim <= 512 ? RowShape{64, 1, 16} : dim <= 2048 ? RowShape{256, 1, 32}
+         : dim <= 4096 ? RowShape{512, 1, 8} : dim <= 8192 ? RowShape{1024, 1, 4} : RowShape{1024, 2, 4};
+}
+// Gradients: each group leaves a row of sums, so few groups with much on their way each (20011 rows of 1001 columns: two groups a
+// compute unit 72 us, four 84; a group per row 82.  20000 of 2048: 86, with a wavefront per row 106).
+constexpr RowShape backward_shape(int dim) {
+    return dim <= 128 ? RowShape{16, 1, 4} : dim <= 512 ? RowShape{64, 1, 4} : dim <= 1024 ? RowShape{64, 2, 2} : dim <= 2048 ? RowShape{256, 1, 4}
+         : dim <= 4096 ? RowShape{512, 1, 2} : dim <= 8192 ? RowShape{1024, 1, 1} : RowShape{1024, 2, 1};
+}
+// Calls f with a shape's lanes and stretches.
+template <class F> hipError_t with_shape(const RowShape& s, F f) {
     using std::integral_constant;
-    if (dim <= 128) return f(integral_constant<int, 16>(), integral_constant<int, 1>());
-    if (dim <= 512) return f(integral_constant<int, 64>(), integral_constant<int, 1>());
-    if (dim <= 1024) return f(integral_constant<int, 64>(), integral_constant<int, 2>());
-    if (dim <= 2048) return f(integral_constant<int, 64>(), integral_constant<int, 4>());
-    if (dim <= 4096) return f(integral_constant<int, 256>(), integral_constant<int, 2>());
-    if (dim <= 8192) return f(integral_constant<int, 256>(), integral_constant<int, 4>());
-    return f(integral_constant<int, 256>(), integral_constant<int, 8>());
+    if (s.lanes == 16) return f(integral_constant<int, 16>(), integral_constant<int, 1>());
+    if (s.lanes == 64 && s.vecs == 1) return f(integral_constant<int, 64>(), integral_constant<int, 1>());
+    if (s.lanes == 64) return f(integral_constant<int, 64>(), integral_constant<int, 2>());
+    if (s.lanes == 256) return f(integral_constant<int, 256>(), integral_constant<int, 1>());
+    if (s.lanes == 512) return f(integral_constant<int, 512>(), integral_constant<int, 1>());
+    if (s.vecs == 1) return f(integral_constant<int, 1024>(), integral_constant<int, 1>());
+    return f(integral_constant<int, 1024>(), integral_constant<int, 2>());
 }
-// Work groups that go through the rows together: as many as there are rows for, `most` per compute unit.
-int norm_groups(int64_t n_rows, int dim, int n_cu, int most) {
-    const int per_group = kThreads / (dim <= 128 ? 16 : dim <= 2048 ? 64 : 256);
-    const int64_t groups = (n_rows + per_group - 1) / per_group;
-    return (int)(groups < (int64_t)most * n_cu ? groups : (int64_t)most * n_cu);
+int row_groups(int64_t n_rows, const RowShape& s, int n_cu) {
+    const int64_t rows = s.lanes < 256 ? 256 / s.lanes : 1, groups = (n_rows + rows - 1) / rows, most = (int64_t)s.groups * n_cu;
+    return (int)(groups < most ? groups : most);
 }
-constexpr int kForwardGroups = 8, kBackwardGroups = 4;
 
 }  // namespace
 
 hipError_t launch_norm(hipStream_t s, const NormArgs& a, int n_cu) {
     return with_type(a.cfg.dtype, [&](auto t) {
-        return with_row(a.cfg.dim, [&](auto tpr, auto nv) {
-            norm_kernel<decltype(t), tpr.value, nv.value><<<dim3((unsigned)norm_groups(a.n_rows, a.cfg.dim, n_cu, kForwardGroups)), dim3(kThreads), 0, s>>>(a);
+        const RowShape shape = forward_shape(a.cfg.dim);
+        return with_shape(shape, [&](auto tpr, auto nv) {
+            norm_kernel<decltype(t), tpr.value, nv.value><<<dim3((unsigned)row_groups(a.n_rows, shape, n_cu)), dim3(kThreads<tpr.value>), 0, s>>>(a);
             return hipGetLastError();
         });
     });
 }
 
-int norm_partials(int64_t n_rows, int dim, int n_cu) { return norm_groups(n_rows, dim, n_cu, kBackwardGroups); }
+int norm_partials(int64_t n_rows, int dim, int n_cu) { return row_groups(n_rows, backward_shape(dim), n_cu); }
 
 hipError_t launch_norm_backward(hipStream_t s, const NormBackArgs& a, int n_cu) {
     const int groups = norm_partials(a.n_rows, a.dim, n_cu);
     hipError_t e = with_type(a.dtype, [&](auto t) {
-        return with_row(a.dim, [&](auto tpr, auto nv) {
-            norm_backward_kernel<decltype(t), tpr.value, nv.value><<<dim3((unsigned)groups), dim3(kThreads), 0, s>>>(a);
+        return with_shape(backward_shape(a.dim), [&](auto tpr, auto nv) {
+            norm_backward_kernel<decltype(t), tpr.value, nv.value><<<dim3((unsigned)groups), dim3(kThreads<tpr.value>), 0, s>>>(a);
             return hipGetLastError();
         });
     });
