@@ -76,6 +76,7 @@ struct ShortConvArgs {
     float* dbias;
     float* partial;                      // [short_conv_partials][dim * (taps + 1)]: by the weight, then by the bias
 };
+int short_conv_tiles(const aug_short_conv_cfg& cfg, bool backward);            // groups of threads across a row
 int short_conv_lg_block(const aug_short_conv_cfg& cfg, bool backward);       // rows of a block, as a power of two
 int short_conv_partials(const aug_short_conv_cfg& cfg, int n_items, int n_cu);
 hipError_t launch_short_conv(hipStream_t s, const ShortConvArgs& a);
