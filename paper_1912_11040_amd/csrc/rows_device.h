@@ -1,10 +1,14 @@
 // Elements, rows and activations on the device, shared by the operators on feature rows.
 #pragma once
 
+#include <type_traits>
+
 #include "rows_internal.h"
 
 namespace aug {
 
+// Calls f with whether no lane's stretch ends outside the row.
+template <class F> hipError_t with_full(bool full, F f) { return full ? f(std::true_type()) : f(std::false_type()); }
 // Calls f with a value of the element type.
 template <class F> hipError_t with_type(int dtype, F f) {
     return dtype == AUG_BF16 ? f((__bf16)0) : dtype == AUG_F16 ? f((_Float16)0) : f(0.f);
@@ -36,6 +40,21 @@ template <class T, int N> __device__ inline void store_pack(T* p, const Pack<T, 
 #pragma unroll
     for (int i = 0; i < N; ++i)
         if (i < valid) p[i] = r.v[i];
+}
+
+// A stretch of channels of row r.  FULL: all of it is there, one access without a branch; else `valid` elements of it.
+template <class T, int VE, bool FULL> __device__ inline Pack<T, VE> load_part(const aug_rows& m, int64_t r, int col, int valid) {
+    if constexpr (FULL) {
+        Pack<T, VE> v;
+        __builtin_memcpy(v.v, row_in<T>(m, r) + col, sizeof v);
+        return v;
+    } else {
+        return load_pack<T, VE>(row_in<T>(m, r) + col, valid);
+    }
+}
+template <class T, int VE, bool FULL> __device__ inline void store_part(const aug_rows& m, int64_t r, int col, const Pack<T, VE>& v, int valid) {
+    if constexpr (FULL) __builtin_memcpy(row_out<T>(m, r) + col, v.v, sizeof v);
+    else store_pack<T, VE>(row_out<T>(m, r) + col, v, valid);
 }
 
 // The sum over LN (a power of two) neighbouring lanes, in all of them: quads by permutation, then mirrored halves and swapped rows, whose

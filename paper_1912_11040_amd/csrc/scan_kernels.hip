@@ -36,25 +36,26 @@ template <int LN, int K> struct Tile {
 
 enum ScanMode { kWhole, kSums, kResume };                // the block is a sequence; its end state from zero and its steps' sum; from its first state
 
-template <class T, int LN, int K, int MODE>
-__global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, float* first_state, float* step_sum) {
+template <class T, int LN, int K, int MODE, bool FULL>
+__global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int all_tiles, float* first_state, float* step_sum) {
     using G = Tile<LN, K>;
     __shared__ float2 su[G::TT][G::CW];                  // (step, step u)
     __shared__ float sb[G::TT][G::NP], sc[MODE == kSums ? 1 : G::TT][G::NP];
     __shared__ float sy[MODE == kSums ? 1 : G::TT][G::YP];
     const int tid = threadIdx.x, dim = a.cfg.dim, n_state = a.cfg.n_state, per_group = dim / a.cfg.n_group;
-    const int tiles = (per_group + G::CW - 1) / G::CW, group = blockIdx.x / tiles, in_group = (blockIdx.x % tiles) * G::CW;
-    const int d0 = group * per_group + in_group, width = min(G::CW, per_group - in_group);
-    const int2 item = a.rows.items[blockIdx.y];
+    const int tile = blockIdx.x % all_tiles, block = blockIdx.x / all_tiles;
+    const int tiles = (per_group + G::CW - 1) / G::CW, group = tile / tiles, in_group = (tile % tiles) * G::CW;
+    const int d0 = group * per_group + in_group, width = FULL ? G::CW : min(G::CW, per_group - in_group);
+    const int2 item = a.rows.items[block];
     const int64_t seq = item.x, begin = a.rows.begin[seq] + ((int64_t)item.y << a.rows.lg), end = a.rows.end[seq];
-    const bool last = a.rows.lg == kWholeLg || blockIdx.y + 1 == gridDim.y || a.rows.items[blockIdx.y + 1].y == 0;
+    const bool last = a.rows.lg == kWholeLg || block + 1 == a.rows.n_items || a.rows.items[block + 1].y == 0;
     if (MODE == kSums && last) return;                   // nobody asks for a sequence's last sums
     const int rows = (int)min(end - begin, (int64_t)1 << a.rows.lg);
 
     // as a walker: channel and states
     const int ch = tid / LN, nq = (tid % LN) * K;
     const bool walks = ch < width;
-    const int64_t at = walks ? ((MODE == kWhole ? seq : (int64_t)blockIdx.y) * dim + d0 + ch) * n_state : 0;
+    const int64_t at = walks ? ((MODE == kWhole ? seq : (int64_t)block) * dim + d0 + ch) * n_state : 0;
     float h[K], rate[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -76,18 +77,18 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, float* first_stat
     Pack<T, G::EPT> u, delta, z;
     T vb[G::BC], vc[G::BC];
     auto fetch = [&](int t0) {
-        const int64_t r = begin + t0 + lt;
-        const int v = t0 + lt < rows ? valid : 0;
-        u = load_pack<T, G::EPT>(row_in<T>(a.in.u, r) + d0 + lc, v);
-        delta = load_pack<T, G::EPT>(row_in<T>(a.in.delta, r) + d0 + lc, v);
-        if (gate) z = load_pack<T, G::EPT>(row_in<T>(a.in.z, r) + d0 + lc, v);
+        const int64_t r = begin + min(t0 + lt, rows - 1);                  // (rows behind the block are not walked)
+        u = load_part<T, G::EPT, FULL>(a.in.u, r, d0 + lc, valid);
+        delta = load_part<T, G::EPT, FULL>(a.in.delta, r, d0 + lc, valid);
+        if (gate) z = load_part<T, G::EPT, FULL>(a.in.z, r, d0 + lc, valid);
 #pragma unroll
         for (int j = 0; j < G::BC; ++j) {
             const int e = tid + 256 * j, t = t0 + e / G::NP, n = e % G::NP;
-            const bool there = e < G::TT * G::NP && t < rows && n < n_state;
-            const int64_t col = (int64_t)group * n_state + n;
-            vb[j] = there ? row_in<T>(a.in.b, begin + t)[col] : (T)0;
-            if (MODE != kSums) vc[j] = there ? row_in<T>(a.in.c, begin + t)[col] : (T)0;
+            const bool there = e < G::TT * G::NP && n < n_state;
+            const int64_t col = (int64_t)group * n_state + min(n, n_state - 1), at = begin + min(t, rows - 1);
+            const T b = row_in<T>(a.in.b, at)[col], c = MODE != kSums ? row_in<T>(a.in.c, at)[col] : (T)0;
+            vb[j] = there ? b : (T)0;
+            vc[j] = there ? c : (T)0;
         }
     };
     float sum = 0.f;
@@ -156,7 +157,7 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, float* first_stat
             }
 #pragma unroll
             for (int i = 0; i < G::EPT; ++i) out.v[i] = (T)p[i];
-            store_pack<T, G::EPT>(row_out<T>(a.y, begin + t0 + lt) + d0 + lc, out, valid);
+            store_part<T, G::EPT, FULL>(a.y, begin + t0 + lt, d0 + lc, out, valid);
         }
     }
     if (!walks) return;
@@ -164,7 +165,7 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, float* first_stat
 #pragma unroll
         for (int k = 0; k < K; ++k)
             if (nq + k < n_state) first_state[at + nq + k] = h[k];
-        if (tid % LN == 0) step_sum[(int64_t)blockIdx.y * dim + d0 + ch] = sum;
+        if (tid % LN == 0) step_sum[(int64_t)block * dim + d0 + ch] = sum;
     } else if (a.state_out && last) {
         float* const out = a.state_out + (seq * dim + d0 + ch) * n_state;
 #pragma unroll
@@ -343,34 +344,34 @@ template <int APART, int EPT> __device__ inline void sum_rows(float (&v)[2 * EPT
     }
 }
 
-template <class T, int LN, int K>
-__global__ __launch_bounds__(256) void scan_back_sums_kernel(ScanArgs a, BackWs ws) {
+template <class T, int LN, int K, bool FULL>
+__global__ __launch_bounds__(256) void scan_back_sums_kernel(ScanArgs a, BackWs ws, int all_tiles) {
     using G = BackTile<LN, K>;
     __shared__ float2 su[G::RT][G::CW];
     __shared__ float sdp[G::RT][G::CW];
     __shared__ float sb[G::RT][G::NP], sc[G::RT][G::NP];
     const int tid = threadIdx.x, dim = a.cfg.dim, n_state = a.cfg.n_state, per_group = dim / a.cfg.n_group;
-    const int tiles = (per_group + G::CW - 1) / G::CW, group = blockIdx.x / tiles, in_group = (blockIdx.x % tiles) * G::CW;
-    const int d0 = group * per_group + in_group, width = min(G::CW, per_group - in_group);
-    const int2 item = a.rows.items[blockIdx.y];
+    const int tile = blockIdx.x % all_tiles, block = blockIdx.x / all_tiles;
+    const int tiles = (per_group + G::CW - 1) / G::CW, group = tile / tiles, in_group = (tile % tiles) * G::CW;
+    const int d0 = group * per_group + in_group, width = FULL ? G::CW : min(G::CW, per_group - in_group);
+    const int2 item = a.rows.items[block];
     const int64_t begin = a.rows.begin[item.x] + ((int64_t)item.y << G::LG), end = a.rows.end[item.x];
     const int here = (int)min(end - begin, (int64_t)G::RT);
     if (here <= 0) return;
-    const int lt = tid / (G::CW / G::EPT), lc = tid % (G::CW / G::EPT) * G::EPT, valid = lt < here ? width - lc : 0;
-    const int64_t r = begin + lt;
-    const auto u = load_pack<T, G::EPT>(row_in<T>(a.in.u, r) + d0 + lc, valid);
-    const auto delta = load_pack<T, G::EPT>(row_in<T>(a.in.delta, r) + d0 + lc, valid);
-    const auto dy = load_pack<T, G::EPT>(row_in<T>(a.dy, r) + d0 + lc, valid);
+    const int lt = tid / (G::CW / G::EPT), lc = tid % (G::CW / G::EPT) * G::EPT, valid = width - lc;
+    const int64_t r = begin + min(lt, here - 1);         // (rows behind the block are not walked)
+    const auto u = load_part<T, G::EPT, FULL>(a.in.u, r, d0 + lc, valid), delta = load_part<T, G::EPT, FULL>(a.in.delta, r, d0 + lc, valid);
+    const auto dy = load_part<T, G::EPT, FULL>(a.dy, r, d0 + lc, valid);
     Pack<T, G::EPT> z;
-    if (a.in.z.data) z = load_pack<T, G::EPT>(row_in<T>(a.in.z, r) + d0 + lc, valid);
+    if (a.in.z.data) z = load_part<T, G::EPT, FULL>(a.in.z, r, d0 + lc, valid);
 #pragma unroll
     for (int j = 0; j < G::BC; ++j) {
         const int e = tid + 256 * j, t = e / G::NP, n = e % G::NP;
         if (t >= G::RT) break;
-        const bool there = t < here && n < n_state;
-        const int64_t col = (int64_t)group * n_state + n;
-        sb[t][n] = there ? (float)row_in<T>(a.in.b, begin + t)[col] : 0.f;
-        sc[t][n] = there ? (float)row_in<T>(a.in.c, begin + t)[col] : 0.f;
+        const int64_t col = (int64_t)group * n_state + min(n, n_state - 1), at = begin + min(t, here - 1);
+        const float b = (float)row_in<T>(a.in.b, at)[col], c = (float)row_in<T>(a.in.c, at)[col];
+        sb[t][n] = n < n_state ? b : 0.f;
+        sc[t][n] = n < n_state ? c : 0.f;
     }
     float raw[G::EPT], step[G::EPT], dp[G::EPT];
 #pragma unroll
@@ -391,7 +392,7 @@ __global__ __launch_bounds__(256) void scan_back_sums_kernel(ScanArgs a, BackWs 
     __syncthreads();
     const int ch = tid / LN, nq = (tid % LN) * K;
     if (ch >= width) return;
-    const int64_t at = ((int64_t)blockIdx.y * dim + d0 + ch) * n_state + nq;
+    const int64_t at = ((int64_t)block * dim + d0 + ch) * n_state + nq;
     float f[K] = {}, q[K], back[K] = {}, rate[K], sum = 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -414,7 +415,7 @@ __global__ __launch_bounds__(256) void scan_back_sums_kernel(ScanArgs a, BackWs 
 #pragma unroll
     for (int k = 0; k < K; ++k)
         if (nq + k < n_state) ws.first[at + k] = f[k], ws.behind[at + k] = back[k];
-    if (tid % LN == 0) ws.steps[(int64_t)blockIdx.y * dim + d0 + ch] = sum;
+    if (tid % LN == 0) ws.steps[(int64_t)block * dim + d0 + ch] = sum;
 }
 
 // Forward through a sequence's blocks for their first states, back for what comes in from behind.
@@ -444,7 +445,7 @@ template <int K> struct RowIn {
 };
 __device__ inline void stay_ahead() { __builtin_amdgcn_sched_barrier(0x2 | 0x4 | 0x200); }      // arithmetic and LDS writes may pass, reads not
 
-template <class T, int LN, int K>
+template <class T, int LN, int K, bool FULL>
 __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs a, BackWs ws, BackPlan plan, int64_t n_rows, bool joined) {
     using G = BackTile<LN, K>;
     constexpr int NS = G::RT / G::SUB, V = 2 * K;
@@ -457,7 +458,7 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
     const int tid = threadIdx.x, dim = a.cfg.dim, n_state = a.cfg.n_state, per_group = dim / a.cfg.n_group;
     const int tile = blockIdx.x % plan.tiles, run = blockIdx.x / plan.tiles;
     const int tiles = plan.tiles / a.cfg.n_group, group = tile / tiles, in_group = (tile % tiles) * G::CW;
-    const int d0 = group * per_group + in_group, width = min(G::CW, per_group - in_group);
+    const int d0 = group * per_group + in_group, width = FULL ? G::CW : min(G::CW, per_group - in_group);
     const int first_item = (int)((int64_t)a.rows.n_items * run / plan.runs), end_item = (int)((int64_t)a.rows.n_items * (run + 1) / plan.runs);
 
     const int ch = tid / LN, nq = (tid % LN) * K, wave = tid / 64;
@@ -493,19 +494,19 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
     };
     auto fetch = [&](const Block& blk, int it, Data& v) {
         if (blk.here <= 0) return;
-        const int valid = lt < blk.here ? width - lc : 0;
-        const int64_t r = blk.begin + lt;
-        v.u = load_pack<T, G::EPT>(row_in<T>(a.in.u, r) + d0 + lc, valid);
-        v.delta = load_pack<T, G::EPT>(row_in<T>(a.in.delta, r) + d0 + lc, valid);
-        v.dy = load_pack<T, G::EPT>(row_in<T>(a.dy, r) + d0 + lc, valid);
-        if (gate) v.z = load_pack<T, G::EPT>(row_in<T>(a.in.z, r) + d0 + lc, valid);
+        const int64_t r = blk.begin + min(lt, blk.here - 1);
+        v.u = load_part<T, G::EPT, FULL>(a.in.u, r, d0 + lc, width - lc);
+        v.delta = load_part<T, G::EPT, FULL>(a.in.delta, r, d0 + lc, width - lc);
+        v.dy = load_part<T, G::EPT, FULL>(a.dy, r, d0 + lc, width - lc);
+        if (gate) v.z = load_part<T, G::EPT, FULL>(a.in.z, r, d0 + lc, width - lc);
 #pragma unroll
         for (int j = 0; j < G::BC; ++j) {
             const int e = tid + 256 * j, t = e / G::NP, n = e % G::NP;
             const bool there = t < blk.here && n < n_state;
-            const int64_t col = (int64_t)group * n_state + n;
-            v.b[j] = there ? row_in<T>(a.in.b, blk.begin + t)[col] : (T)0;
-            v.c[j] = there ? row_in<T>(a.in.c, blk.begin + t)[col] : (T)0;
+            const int64_t col = (int64_t)group * n_state + min(n, n_state - 1), at = blk.begin + min(t, blk.here - 1);
+            const T b = row_in<T>(a.in.b, at)[col], c = row_in<T>(a.in.c, at)[col];
+            v.b[j] = there ? b : (T)0;
+            v.c[j] = there ? c : (T)0;
         }
         // the state before the block, and what comes in from behind it: e g of the row behind
         const int64_t at = ((int64_t)it * dim + d0 + ch) * n_state + nq, in = ((int64_t)blk.seq * dim + d0 + ch) * n_state + nq;
@@ -556,9 +557,10 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
         }
 #pragma unroll
         for (int i = 0; i < G::EPT; ++i) {
+            // (rows behind the sequence are walked with steps and dp of zero)
             step[i] = i < valid ? step[i] : 0.f;
-            su[lt][lc + i] = make_float2(step[i], step[i] * (float)u.v[i]);
-            sdp[lt][lc + i] = dp[i];
+            su[lt][lc + i] = make_float2(step[i], i < valid ? step[i] * (float)u.v[i] : 0.f);
+            sdp[lt][lc + i] = i < valid ? dp[i] : 0.f;
         }
         __syncthreads();
         // states before the later stretches
@@ -693,9 +695,11 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
             par[i] = i < valid ? dp[i] * (float)u.v[i] : 0.f;
             par[G::EPT + i] = i < valid ? dstep[i] : 0.f;
         }
-        if (a.grad.du.data) store_pack<T, G::EPT>(row_out<T>(a.grad.du, r) + d0 + lc, du, valid);
-        if (a.grad.ddelta.data) store_pack<T, G::EPT>(row_out<T>(a.grad.ddelta, r) + d0 + lc, dd, valid);
-        if (a.grad.dz.data) store_pack<T, G::EPT>(row_out<T>(a.grad.dz, r) + d0 + lc, dz, valid);
+        if (lt < here) {
+            if (a.grad.du.data) store_part<T, G::EPT, FULL>(a.grad.du, r, d0 + lc, du, valid);
+            if (a.grad.ddelta.data) store_part<T, G::EPT, FULL>(a.grad.ddelta, r, d0 + lc, dd, valid);
+            if (a.grad.dz.data) store_part<T, G::EPT, FULL>(a.grad.dz, r, d0 + lc, dz, valid);
+        }
         sum_rows<G::CW / G::EPT, G::EPT>(par);
 #pragma unroll
         for (int i = 0; i < kept<G::EPT>(); ++i) acc[i] += par[i];
@@ -752,6 +756,11 @@ __global__ __launch_bounds__(256) void scan_bc_kernel(ScanArgs a, BackWs ws, Bac
 
 }  // namespace
 
+template <class F> void with_groups(bool eight, F f) {
+    if (eight) f(std::integral_constant<int, 8>());
+    else f(std::integral_constant<int, 1>());
+}
+
 // Calls f with the lanes per channel and the states per lane for so many states, as integral constants.
 template <class F> hipError_t with_lanes(int n_state, F f) {
     using std::integral_constant;
@@ -784,11 +793,6 @@ int scan_lg_block(const aug_scan_cfg& cfg, int n_seq, const int64_t* begin, cons
     while (lg > 6 && (rows >> lg) * tiles < 4 * (int64_t)n_cu) --lg;
     return lg;
 }
-template <class F> void with_groups(bool eight, F f) {
-    if (eight) f(std::integral_constant<int, 8>());
-    else f(std::integral_constant<int, 1>());
-}
-
 // The gradients' lanes: at least four per channel, so that a block's elements are eight to a lane at most.
 template <class F> hipError_t with_back_lanes(int n_state, F f) {
     using std::integral_constant;
@@ -817,28 +821,31 @@ size_t scan_workspace(const aug_scan_cfg& cfg, int n_items, int64_t n_rows, int 
 }
 
 hipError_t launch_scan(hipStream_t s, const ScanArgs& a, int n_cu) {
+    const int tiles = scan_tiles(a.cfg);
     return with_type(a.cfg.dtype, [&](auto t) {
         return with_lanes(a.cfg.n_state, [&](auto ln, auto k) {
-            using T = decltype(t);
-            const dim3 grid((unsigned)scan_tiles(a.cfg), (unsigned)a.rows.n_items);
-            float* const first_state = static_cast<float*>(a.ws);
-            float* const step_sum = first_state + (int64_t)a.rows.n_items * a.cfg.dim * a.cfg.n_state;
-            if (a.rows.lg == kWholeLg) {
-                scan_kernel<T, ln.value, k.value, kWhole><<<grid, dim3(256), 0, s>>>(a, nullptr, nullptr);
+            return with_full(a.cfg.dim / a.cfg.n_group % (256 / ln.value) == 0, [&](auto full) {
+                using T = decltype(t);
+                const dim3 grid((unsigned)(tiles * a.rows.n_items));
+                float* const first_state = static_cast<float*>(a.ws);
+                float* const step_sum = first_state + (int64_t)a.rows.n_items * a.cfg.dim * a.cfg.n_state;
+                if (a.rows.lg == kWholeLg) {
+                    scan_kernel<T, ln.value, k.value, kWhole, full.value><<<grid, dim3(256), 0, s>>>(a, tiles, nullptr, nullptr);
+                    return hipGetLastError();
+                }
+                scan_kernel<T, ln.value, k.value, kSums, full.value><<<grid, dim3(256), 0, s>>>(a, tiles, first_state, step_sum);
+                hipError_t e = hipGetLastError();
+                if (e != hipSuccess) return e;
+                const int64_t width = (int64_t)a.cfg.dim * a.cfg.n_state;
+                with_groups(join_in_groups(width, a.rows.n_seq, a.rows.n_items, n_cu), [&](auto g) {
+                    constexpr int n = kJoinStates<g.value>;
+                    scan_join_kernel<g.value><<<dim3((unsigned)((width + n - 1) / n), (unsigned)a.rows.n_seq), dim3(n * g.value), 0, s>>>(a, first_state, step_sum);
+                });
+                e = hipGetLastError();
+                if (e != hipSuccess) return e;
+                scan_kernel<T, ln.value, k.value, kResume, full.value><<<grid, dim3(256), 0, s>>>(a, tiles, first_state, step_sum);
                 return hipGetLastError();
-            }
-            scan_kernel<T, ln.value, k.value, kSums><<<grid, dim3(256), 0, s>>>(a, first_state, step_sum);
-            hipError_t e = hipGetLastError();
-            if (e != hipSuccess) return e;
-            const int64_t width = (int64_t)a.cfg.dim * a.cfg.n_state;
-            with_groups(join_in_groups(width, a.rows.n_seq, a.rows.n_items, n_cu), [&](auto g) {
-                constexpr int n = kJoinStates<g.value>;
-                scan_join_kernel<g.value><<<dim3((unsigned)((width + n - 1) / n), (unsigned)a.rows.n_seq), dim3(n * g.value), 0, s>>>(a, first_state, step_sum);
             });
-            e = hipGetLastError();
-            if (e != hipSuccess) return e;
-            scan_kernel<T, ln.value, k.value, kResume><<<grid, dim3(256), 0, s>>>(a, first_state, step_sum);
-            return hipGetLastError();
         });
     });
 }
@@ -865,19 +872,21 @@ hipError_t launch_scan_backward(hipStream_t s, const ScanArgs& a, int64_t n_rows
     hipError_t e = with_type(a.cfg.dtype, [&](auto t) {
         return with_back_lanes(a.cfg.n_state, [&](auto ln, auto k) {
             using T = decltype(t);
-            if (joined) {
-                scan_back_sums_kernel<T, ln.value, k.value><<<dim3((unsigned)plan.tiles, (unsigned)a.rows.n_items), dim3(256), 0, s>>>(a, ws);
-                hipError_t e = hipGetLastError();
-                if (e != hipSuccess) return e;
-                with_groups(join_in_groups(width, a.rows.n_seq, a.rows.n_items, n_cu), [&](auto g) {
-                constexpr int n = kJoinStates<g.value>;
-                scan_back_join_kernel<g.value><<<dim3((unsigned)((width + n - 1) / n), (unsigned)a.rows.n_seq), dim3(n * g.value), 0, s>>>(a, ws);
+            hipError_t e = with_full(a.cfg.dim / a.cfg.n_group % (256 / ln.value) == 0, [&](auto full) {
+                if (joined) {
+                    scan_back_sums_kernel<T, ln.value, k.value, full.value><<<dim3((unsigned)(plan.tiles * a.rows.n_items)), dim3(256), 0, s>>>(a, ws, plan.tiles);
+                    hipError_t e = hipGetLastError();
+                    if (e != hipSuccess) return e;
+                    with_groups(join_in_groups(width, a.rows.n_seq, a.rows.n_items, n_cu), [&](auto g) {
+                        constexpr int n = kJoinStates<g.value>;
+                        scan_back_join_kernel<g.value><<<dim3((unsigned)((width + n - 1) / n), (unsigned)a.rows.n_seq), dim3(n * g.value), 0, s>>>(a, ws);
+                    });
+                    e = hipGetLastError();
+                    if (e != hipSuccess) return e;
+                }
+                scan_back_kernel<T, ln.value, k.value, full.value><<<dim3((unsigned)(plan.tiles * plan.runs)), dim3(256), 0, s>>>(a, ws, plan, n_rows, joined);
+                return hipGetLastError();
             });
-                e = hipGetLastError();
-                if (e != hipSuccess) return e;
-            }
-            scan_back_kernel<T, ln.value, k.value><<<dim3((unsigned)(plan.tiles * plan.runs)), dim3(256), 0, s>>>(a, ws, plan, n_rows, joined);
-            hipError_t e = hipGetLastError();
             if (e != hipSuccess || (!a.grad.db.data && !a.grad.dc.data)) return e;
             scan_bc_kernel<T><<<dim3((unsigned)a.rows.n_items), dim3(256), 0, s>>>(a, ws, plan, n_rows);
             return hipGetLastError();

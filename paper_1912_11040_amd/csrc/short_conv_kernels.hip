@@ -34,21 +34,6 @@ int lg_rows(const aug_short_conv_cfg& cfg, int vec, int rows) {      // of a gro
     return lg;
 }
 
-// A stretch of channels of row r.  FULL: all of it is there, one access without a branch; else `valid` elements of it.
-template <class T, int VE, bool FULL> __device__ inline Pack<T, VE> load_part(const aug_rows& m, int64_t r, int col, int valid) {
-    if constexpr (FULL) {
-        Pack<T, VE> v;
-        __builtin_memcpy(v.v, row_in<T>(m, r) + col, sizeof v);
-        return v;
-    } else {
-        return load_pack<T, VE>(row_in<T>(m, r) + col, valid);
-    }
-}
-template <class T, int VE, bool FULL> __device__ inline void store_part(const aug_rows& m, int64_t r, int col, const Pack<T, VE>& v, int valid) {
-    if constexpr (FULL) __builtin_memcpy(row_out<T>(m, r) + col, v.v, sizeof v);
-    else store_pack<T, VE>(row_out<T>(m, r) + col, v, valid);
-}
-
 // Rows t < 0 are those of the state (or zeros), oldest first.
 template <class T, int VE>
 __device__ inline Pack<T, VE> row_before(const ShortConvArgs& a, int seq, int64_t t, int col, int valid) {
@@ -292,8 +277,6 @@ template <class F> hipError_t with_taps(int taps, F f) {
         default: return f(integral_constant<int, 8>());
     }
 }
-// Calls f with whether no lane's stretch ends outside the row.
-template <class F> hipError_t with_full(bool full, F f) { return full ? f(std::true_type()) : f(std::false_type()); }
 
 }  // namespace
 
