@@ -43,37 +43,18 @@ class VtlpCfg(ctypes.Structure):
     _fields_ = [("win", ctypes.c_int), ("hop", ctypes.c_int), ("nfft", ctypes.c_int)]
 
 
-class Rows(ctypes.Structure):
-    """Mirror of aug_rows."""
-    _fields_ = [("data", ctypes.c_void_p), ("ld", ctypes.c_int64)]
+# The C structs of the operators on feature rows as arrays of their fields, which is the cheapest way to fill them: a call for a few
+# streams takes the GPU four microseconds.
+ROWS = ctypes.c_int64 * 2               # aug_rows: data, ld
+SCAN_IN = ctypes.c_int64 * 13           # aug_scan_in: u, delta, b, c, z (aug_rows each), a, skip, delta_bias
+SCAN_GRAD = ctypes.c_int64 * 13         # aug_scan_grad: du, ddelta, db, dc, dz, da, dskip, ddelta_bias
+SHORT_CONV_CFG = ctypes.c_int * 4       # aug_short_conv_cfg: dtype, dim, taps, silu
+SCAN_CFG = ctypes.c_int * 5             # aug_scan_cfg: dtype, dim, n_state, n_group, softplus
 
 
 class NormCfg(ctypes.Structure):
     """Mirror of aug_norm_cfg."""
     _fields_ = [("dtype", ctypes.c_int), ("dim", ctypes.c_int), ("eps", ctypes.c_float), ("q_block", ctypes.c_int)]
-
-
-class ShortConvCfg(ctypes.Structure):
-    """Mirror of aug_short_conv_cfg."""
-    _fields_ = [("dtype", ctypes.c_int), ("dim", ctypes.c_int), ("taps", ctypes.c_int), ("silu", ctypes.c_int)]
-
-
-class ScanCfg(ctypes.Structure):
-    """Mirror of aug_scan_cfg."""
-    _fields_ = [("dtype", ctypes.c_int), ("dim", ctypes.c_int), ("n_state", ctypes.c_int), ("n_group", ctypes.c_int),
-                ("softplus", ctypes.c_int)]
-
-
-class ScanIn(ctypes.Structure):
-    """Mirror of aug_scan_in."""
-    _fields_ = [("u", Rows), ("delta", Rows), ("b", Rows), ("c", Rows), ("z", Rows), ("a", ctypes.c_void_p),
-                ("skip", ctypes.c_void_p), ("delta_bias", ctypes.c_void_p)]
-
-
-class ScanGrad(ctypes.Structure):
-    """Mirror of aug_scan_grad."""
-    _fields_ = [("du", Rows), ("ddelta", Rows), ("db", Rows), ("dc", Rows), ("dz", Rows), ("da", ctypes.c_void_p),
-                ("dskip", ctypes.c_void_p), ("ddelta_bias", ctypes.c_void_p)]
 
 
 class AugError(RuntimeError):
@@ -138,17 +119,14 @@ def load_library() -> ctypes.CDLL:
     lib.aug_pipeline_batch.argtypes = [vp, ci, p_i64, vp, ci, vp, vp, ci, cf, cf, vp, vp, p_cfg,
                                        p_i64, vp, vp, vp, vp]
     lib.aug_pipeline_batch.restype = ci
-    p_rows = ctypes.POINTER(Rows)
-    lib.aug_rms_norm_batch.argtypes = [vp, i64, ctypes.POINTER(NormCfg), p_rows, p_rows, vp, p_rows, p_rows, p_rows, vp, vp]
-    lib.aug_rms_norm_backward_batch.argtypes = [vp, i64, ctypes.POINTER(NormCfg), p_rows, vp, vp, p_rows, p_rows, p_rows, vp]
-    p_conv = ctypes.POINTER(ShortConvCfg)
-    lib.aug_short_conv_batch.argtypes = [vp, ci, p_i64, p_i64, p_conv, p_rows, vp, vp, vp, vp, p_rows]
-    lib.aug_short_conv_backward_batch.argtypes = [vp, ci, p_i64, p_i64, p_conv, p_rows, vp, vp, vp, p_rows, p_rows, vp, vp]
-    lib.aug_short_conv_step.argtypes = [vp, ci, p_conv, p_rows, vp, vp, vp, vp, p_rows]
-    p_scan, p_in = ctypes.POINTER(ScanCfg), ctypes.POINTER(ScanIn)
-    lib.aug_scan_batch.argtypes = [vp, ci, p_i64, p_i64, p_scan, p_in, vp, vp, p_rows]
-    lib.aug_scan_backward_batch.argtypes = [vp, ci, p_i64, p_i64, p_scan, p_in, vp, p_rows, ctypes.POINTER(ScanGrad)]
-    lib.aug_scan_step.argtypes = [vp, ci, p_scan, p_in, vp, vp, p_rows]
+    lib.aug_rms_norm_batch.argtypes = [vp, i64] + [vp] * 9
+    lib.aug_rms_norm_backward_batch.argtypes = [vp, i64] + [vp] * 8
+    lib.aug_short_conv_batch.argtypes = [vp, ci] + [vp] * 9
+    lib.aug_short_conv_backward_batch.argtypes = [vp, ci] + [vp] * 11
+    lib.aug_short_conv_step.argtypes = [vp, ci] + [vp] * 7
+    lib.aug_scan_batch.argtypes = [vp, ci] + [vp] * 7
+    lib.aug_scan_backward_batch.argtypes = [vp, ci] + [vp] * 7
+    lib.aug_scan_step.argtypes = [vp, ci] + [vp] * 5
     for name in EXPORTS:
         if name.startswith(("aug_rms_norm", "aug_short_conv", "aug_scan")):
             getattr(lib, name).restype = ci
@@ -270,6 +248,12 @@ def _element_types():
     return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}      # AUG_F32, AUG_BF16, AUG_F16
 
 
+@functools.lru_cache(maxsize=None)
+def _float32():
+    import torch
+    return torch.float32
+
+
 def _element_type(t) -> int:
     try:
         return _element_types()[t.dtype]
@@ -277,16 +261,31 @@ def _element_type(t) -> int:
         raise TypeError(f"expected float32, bfloat16 or float16, got {t.dtype}") from None
 
 
-def check_matrix(name: str, t, n_rows: int, width: int, dtype=None):
-    """Raise unless `t` has at least n_rows rows of exactly `width` columns next to each other."""
-    if t.dim() != 2 or t.shape[0] < n_rows or t.shape[1] != width:
-        raise ValueError(f"{name} is {tuple(t.shape)}, the call needs {n_rows} rows of {width}")
-    if width > 1 and t.stride(1) != 1:
-        raise ValueError(f"the columns of {name} are not next to each other")
-    if t.shape[0] > 1 and t.stride(0) < width:
-        raise ValueError(f"the rows of {name} overlap")
-    if dtype is not None and t.dtype != dtype:
+def check_matrix(name: str, t, n_rows: int, width: int, dtype) -> int:
+    """Raise unless `t` has at least n_rows rows of exactly `width` columns next to each other; its leading dimension."""
+    shape = t.shape
+    if len(shape) != 2 or shape[0] < n_rows or shape[1] != width:
+        raise ValueError(f"{name} is {tuple(shape)}, the call needs {n_rows} rows of {width}")
+    if t.dtype != dtype:
         raise TypeError(f"{name} is {t.dtype}, expected {dtype}")
+    down, across = t.stride()
+    if across != 1 and width > 1:
+        raise ValueError(f"the columns of {name} are not next to each other")
+    if shape[0] <= 1:
+        return width
+    if down < width:
+        raise ValueError(f"the rows of {name} overlap")
+    return down
+
+
+def check_array(name: str, t, count: int, dtype):
+    """Raise unless `t` is a contiguous tensor of exactly `count` elements."""
+    if t.numel() != count:
+        raise ValueError(f"{name} holds {t.numel()} elements, the call needs exactly {count}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} is {t.dtype}, expected {dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
 
 
 def check_row_offsets(off: np.ndarray, lengths: Optional[np.ndarray] = None) -> int:
@@ -299,64 +298,10 @@ def check_row_offsets(off: np.ndarray, lengths: Optional[np.ndarray] = None) -> 
     return int((off[:-1] + lengths).max(initial=0))
 
 
-def check_norm_sizes(x, weight, matrices, q_out=None, scale_out=None, q_block: int = 0, per_row=()):
-    """matrices and per_row: (name, tensor or None) pairs of x's shape, and of a float per row."""
-    if x.dim() != 2:
-        raise ValueError("x must have two dimensions")
-    n_rows, dim = x.shape
-    check_matrix("x", x, n_rows, dim)
-    for name, t in matrices:
-        if t is not None:
-            check_matrix(name, t, n_rows, dim, x.dtype)
-    if weight is not None:
-        _need("weight", weight, dim, exact=True)
-    if q_out is not None:
-        check_matrix("q_out", q_out, n_rows, dim)
-        if q_out.element_size() != 1:
-            raise TypeError(f"q_out is {q_out.dtype}, expected an 8-bit type")
-        _need("scale_out", scale_out, n_rows * (-(-dim // q_block) if q_block > 0 else 1))
-    for name, t in per_row:
-        if t is not None:
-            _need(name, t, n_rows)
-
-
-def check_short_conv_sizes(n_seq: int, n_rows: int, x, weight, matrices, bias=None, states=(), dweight_out=None, dbias_out=None):
-    if x.dim() != 2 or weight.dim() != 2 or weight.shape[0] != x.shape[1]:
-        raise ValueError("weight must be [dim][taps] with x's dim")
-    dim, taps = weight.shape
-    check_matrix("x", x, n_rows, dim)
-    for name, t in matrices:
-        if t is not None:
-            check_matrix(name, t, n_rows, dim, x.dtype)
-    for name, t in states:
-        if t is not None:
-            _need(name, t, n_seq * (taps - 1) * dim, exact=True)
-            if t.dtype != x.dtype:
-                raise TypeError(f"{name} is {t.dtype}, expected {x.dtype}")
-    for name, t, count in (("bias", bias, dim), ("dweight_out", dweight_out, dim * taps), ("dbias_out", dbias_out, dim)):
-        if t is not None:
-            _need(name, t, count, exact=True)
-
-
-def check_scan_sizes(n_seq: int, n_rows: int, u, delta, a, b, c, n_group: int, matrices=(), per_group=(), states=(), da_out=None,
-                     per_channel=()):
-    """matrices: of u's shape; per_group: of b's; states: [n_seq][dim][n_state]; per_channel: floats."""
-    if u.dim() != 2 or a.dim() != 2 or a.shape[0] != u.shape[1]:
-        raise ValueError("a must be [dim][n_state] with u's dim")
-    dim, n_state = a.shape
-    check_matrix("u", u, n_rows, dim)
-    for name, t in (("delta", delta), *matrices):
-        if t is not None:
-            check_matrix(name, t, n_rows, dim, u.dtype)
-    for name, t in (("b", b), ("c", c), *per_group):
-        if t is not None:
-            check_matrix(name, t, n_rows, n_group * n_state, u.dtype)
-    for name, t in states:
-        if t is not None:
-            _need(name, t, n_seq * dim * n_state, exact=True)
-    for name, t, count in (("da_out", da_out, dim * n_state), *((name, t, dim) for name, t in per_channel)):
-        if t is not None:
-            _need(name, t, count, exact=True)
+def _two_dimensions(name: str, t):
+    if len(t.shape) != 2:
+        raise ValueError(f"{name} must have two dimensions")
+    return t.shape
 
 
 class Augmenter:
@@ -518,123 +463,123 @@ class Augmenter:
             _ptr(rir_out, torch.float32), _ptr(mixed_out, torch.float32),
             _ptr(gains_out, torch.float32)))
 
-    # ---- operators on feature rows: matrices are [rows][columns] tensors, column slices of wider ones among them ----
+    # ---- operators on feature rows: matrices are [rows][columns] tensors, column slices of wider ones among them.  Their
+    # shapes are checked whatever check_sizes says: the leading dimension comes from them. ----
 
-    def _matrix(self, t):
-        """A matrix argument of the library (None -> an empty one)."""
-        if t is None:
-            return Rows(None, 0)
+    def _on_device(self, name, t):
         if t.get_device() != self.device:
-            raise ValueError(f"expected a tensor on device {self.device}, got {t.device}")
-        return Rows(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1])
+            raise ValueError(f"{name} is on {t.device}, the context on device {self.device}")
+        return t.data_ptr()
 
-    def _array(self, t, dtype=None):
-        if t is not None and t.get_device() != self.device:
-            raise ValueError(f"expected a tensor on device {self.device}, got {t.device}")
-        return _ptr(t, dtype)
+    def _matrix(self, name, t, n_rows, width, dtype):
+        """The fields of aug_rows (None: no matrix)."""
+        if t is None:
+            return 0, 0
+        ld = check_matrix(name, t, n_rows, width, dtype)
+        return self._on_device(name, t), ld
 
-    def _floats(self, t):
-        import torch
-        return self._array(t, torch.float32)
+    def _array(self, name, t, count, dtype=None):
+        if t is None:
+            return None
+        check_array(name, t, count, _float32() if dtype is None else dtype)
+        return self._on_device(name, t)
 
     @staticmethod
     def _sequences(row_offsets, row_lengths):
-        """n_seq, the host arrays and their addresses."""
+        """n_seq, the rows that they reach, and the host arrays with their addresses."""
         off = _host_i64(row_offsets)
         lengths = None if row_lengths is None else _host_i64(row_lengths)
         n_rows = check_row_offsets(off, lengths)
-        p = ctypes.POINTER(ctypes.c_int64)
-        return len(off) - 1, n_rows, (off, lengths), (off.ctypes.data_as(p), None if lengths is None else lengths.ctypes.data_as(p))
+        return len(off) - 1, n_rows, (off, lengths), off.ctypes.data, None if lengths is None else lengths.ctypes.data
 
     def aug_rms_norm_batch(self, x, weight=None, residual=None, eps: float = 1e-6, sum_out=None, y_out=None, q_out=None,
                            scale_out=None, rstd_out=None, q_block: int = 0):
-        if self._check_sizes:
-            check_norm_sizes(x, weight, (("residual", residual), ("sum_out", sum_out), ("y_out", y_out)), q_out, scale_out, q_block,
-                             (("rstd_out", rstd_out),))
-        c = NormCfg(_element_type(x), int(x.shape[1]), float(eps), int(q_block))
-        m = self._matrix
-        self._check(self._lib.aug_rms_norm_batch(self._h, int(x.shape[0]), c, m(x), m(residual), self._floats(weight), m(sum_out),
-                                                 m(y_out), m(q_out), self._floats(scale_out), self._floats(rstd_out)))
+        import torch
+        n_rows, dim = _two_dimensions("x", x)
+        m, arr, dtype = self._matrix, self._array, x.dtype
+        q_type = dtype if q_out is None else q_out.dtype
+        if q_type not in (torch.float8_e4m3fn, torch.uint8) and q_out is not None:
+            raise TypeError(f"q_out is {q_type}, expected float8_e4m3fn (or uint8 for the same bits)")
+        scales = n_rows * (-(-dim // q_block) if q_block > 0 else 1)
+        self._check(self._lib.aug_rms_norm_batch(
+            self._h, n_rows, ctypes.byref(NormCfg(_element_type(x), dim, eps, q_block)), ROWS(*m("x", x, n_rows, dim, dtype)),
+            ROWS(*m("residual", residual, n_rows, dim, dtype)), arr("weight", weight, dim),
+            ROWS(*m("sum_out", sum_out, n_rows, dim, dtype)), ROWS(*m("y_out", y_out, n_rows, dim, dtype)),
+            ROWS(*m("q_out", q_out, n_rows, dim, q_type)), arr("scale_out", scale_out, scales), arr("rstd_out", rstd_out, n_rows)))
 
     def aug_rms_norm_backward_batch(self, x, rstd, dy, weight=None, dsum=None, dx_out=None, dweight_out=None):
         """x is the forward call's sum (its input where there was no residual)."""
-        if self._check_sizes:
-            check_norm_sizes(x, weight, (("dy", dy), ("dsum", dsum), ("dx_out", dx_out)), per_row=(("rstd", rstd),))
-            if dweight_out is not None:
-                _need("dweight_out", dweight_out, x.shape[1], exact=True)
-        c = NormCfg(_element_type(x), int(x.shape[1]), 0.0, 0)
-        m = self._matrix
-        self._check(self._lib.aug_rms_norm_backward_batch(self._h, int(x.shape[0]), c, m(x), self._floats(weight), self._floats(rstd),
-                                                          m(dy), m(dsum), m(dx_out), self._floats(dweight_out)))
+        n_rows, dim = _two_dimensions("x", x)
+        m, arr, dtype = self._matrix, self._array, x.dtype
+        self._check(self._lib.aug_rms_norm_backward_batch(
+            self._h, n_rows, ctypes.byref(NormCfg(_element_type(x), dim, 0.0, 0)), ROWS(*m("x", x, n_rows, dim, dtype)),
+            arr("weight", weight, dim), arr("rstd", rstd, n_rows), ROWS(*m("dy", dy, n_rows, dim, dtype)),
+            ROWS(*m("dsum", dsum, n_rows, dim, dtype)), ROWS(*m("dx_out", dx_out, n_rows, dim, dtype)),
+            arr("dweight_out", dweight_out, dim)))
 
     def aug_short_conv_batch(self, row_offsets, x, weight, y_out, bias=None, activation: str = "silu", state_in=None,
                              state_out=None, row_lengths=None):
-        n_seq, n_rows, _keep, (off, lengths) = self._sequences(row_offsets, row_lengths)
-        if self._check_sizes:
-            check_short_conv_sizes(n_seq, n_rows, x, weight, (("y_out", y_out),), bias, (("state_in", state_in), ("state_out", state_out)))
-        c = ShortConvCfg(_element_type(x), int(weight.shape[0]), int(weight.shape[1]), ACTIVATIONS[activation])
-        m = self._matrix
-        self._check(self._lib.aug_short_conv_batch(self._h, n_seq, off, lengths, c, m(x), self._floats(weight), self._floats(bias),
-                                                   self._array(state_in), self._array(state_out), m(y_out)))
+        n_seq, n_rows, _keep, off, lengths = self._sequences(row_offsets, row_lengths)
+        dim, taps = _two_dimensions("weight", weight)
+        m, arr, dtype, held = self._matrix, self._array, x.dtype, n_seq * (taps - 1) * dim
+        self._check(self._lib.aug_short_conv_batch(
+            self._h, n_seq, off, lengths, SHORT_CONV_CFG(_element_type(x), dim, taps, ACTIVATIONS[activation]),
+            ROWS(*m("x", x, n_rows, dim, dtype)), arr("weight", weight, dim * taps), arr("bias", bias, dim),
+            arr("state_in", state_in, held, dtype), arr("state_out", state_out, held, dtype), ROWS(*m("y_out", y_out, n_rows, dim, dtype))))
 
     def aug_short_conv_backward_batch(self, row_offsets, x, weight, dy, bias=None, activation: str = "silu", state_in=None,
                                       dx_out=None, dweight_out=None, dbias_out=None, row_lengths=None):
-        n_seq, n_rows, _keep, (off, lengths) = self._sequences(row_offsets, row_lengths)
-        if self._check_sizes:
-            check_short_conv_sizes(n_seq, n_rows, x, weight, (("dy", dy), ("dx_out", dx_out)), bias, (("state_in", state_in),),
-                                   dweight_out, dbias_out)
-        c = ShortConvCfg(_element_type(x), int(weight.shape[0]), int(weight.shape[1]), ACTIVATIONS[activation])
-        m = self._matrix
+        n_seq, n_rows, _keep, off, lengths = self._sequences(row_offsets, row_lengths)
+        dim, taps = _two_dimensions("weight", weight)
+        m, arr, dtype = self._matrix, self._array, x.dtype
         self._check(self._lib.aug_short_conv_backward_batch(
-            self._h, n_seq, off, lengths, c, m(x), self._floats(weight), self._floats(bias), self._array(state_in), m(dy), m(dx_out),
-            self._floats(dweight_out), self._floats(dbias_out)))
+            self._h, n_seq, off, lengths, SHORT_CONV_CFG(_element_type(x), dim, taps, ACTIVATIONS[activation]),
+            ROWS(*m("x", x, n_rows, dim, dtype)), arr("weight", weight, dim * taps), arr("bias", bias, dim),
+            arr("state_in", state_in, n_seq * (taps - 1) * dim, dtype), ROWS(*m("dy", dy, n_rows, dim, dtype)),
+            ROWS(*m("dx_out", dx_out, n_rows, dim, dtype)), arr("dweight_out", dweight_out, dim * taps), arr("dbias_out", dbias_out, dim)))
 
     def aug_short_conv_step(self, x, weight, state_in, state_out, y_out, bias=None, activation: str = "silu"):
-        n_seq = int(x.shape[0])
-        if self._check_sizes:
-            check_short_conv_sizes(n_seq, n_seq, x, weight, (("y_out", y_out),), bias, (("state_in", state_in), ("state_out", state_out)))
-        c = ShortConvCfg(_element_type(x), int(weight.shape[0]), int(weight.shape[1]), ACTIVATIONS[activation])
-        self._check(self._lib.aug_short_conv_step(self._h, n_seq, c, self._matrix(x), self._floats(weight), self._floats(bias),
-                                                  self._array(state_in), self._array(state_out), self._matrix(y_out)))
+        n_seq = x.shape[0]
+        dim, taps = _two_dimensions("weight", weight)
+        m, arr, dtype, held = self._matrix, self._array, x.dtype, n_seq * (taps - 1) * dim
+        self._check(self._lib.aug_short_conv_step(
+            self._h, n_seq, SHORT_CONV_CFG(_element_type(x), dim, taps, ACTIVATIONS[activation]), ROWS(*m("x", x, n_seq, dim, dtype)),
+            arr("weight", weight, dim * taps), arr("bias", bias, dim), arr("state_in", state_in, held, dtype),
+            arr("state_out", state_out, held, dtype), ROWS(*m("y_out", y_out, n_seq, dim, dtype))))
 
-    def _scan_in(self, u, delta, a, b, c, skip, z, delta_bias, softplus, n_group):
-        m = self._matrix
-        cfg = ScanCfg(_element_type(u), int(a.shape[0]), int(a.shape[1]), int(n_group), int(bool(softplus)))
-        return cfg, ScanIn(m(u), m(delta), m(b), m(c), m(z), self._floats(a), self._floats(skip), self._floats(delta_bias))
+    def _scan_in(self, n_rows, u, delta, a, b, c, skip, z, delta_bias, softplus, n_group):
+        dim, n_state = _two_dimensions("a", a)
+        m, arr, dtype, group = self._matrix, self._array, u.dtype, n_group * n_state
+        return SCAN_CFG(_element_type(u), dim, n_state, n_group, bool(softplus)), SCAN_IN(
+            *m("u", u, n_rows, dim, dtype), *m("delta", delta, n_rows, dim, dtype), *m("b", b, n_rows, group, dtype),
+            *m("c", c, n_rows, group, dtype), *m("z", z, n_rows, dim, dtype), arr("a", a, dim * n_state),
+            arr("skip", skip, dim) or 0, arr("delta_bias", delta_bias, dim) or 0)
 
     def aug_scan_batch(self, row_offsets, u, delta, a, b, c, y_out, skip=None, z=None, delta_bias=None, softplus: bool = True,
                        n_group: int = 1, state_in=None, state_out=None, row_lengths=None):
-        n_seq, n_rows, _keep, (off, lengths) = self._sequences(row_offsets, row_lengths)
-        if self._check_sizes:
-            check_scan_sizes(n_seq, n_rows, u, delta, a, b, c, n_group, (("z", z), ("y_out", y_out)),
-                             states=(("state_in", state_in), ("state_out", state_out)),
-                             per_channel=(("skip", skip), ("delta_bias", delta_bias)))
-        cfg, ins = self._scan_in(u, delta, a, b, c, skip, z, delta_bias, softplus, n_group)
-        self._check(self._lib.aug_scan_batch(self._h, n_seq, off, lengths, cfg, ins, self._floats(state_in), self._floats(state_out),
-                                             self._matrix(y_out)))
+        n_seq, n_rows, _keep, off, lengths = self._sequences(row_offsets, row_lengths)
+        cfg, ins = self._scan_in(n_rows, u, delta, a, b, c, skip, z, delta_bias, softplus, n_group)
+        arr, held = self._array, n_seq * a.numel()
+        self._check(self._lib.aug_scan_batch(self._h, n_seq, off, lengths, cfg, ins, arr("state_in", state_in, held),
+                                             arr("state_out", state_out, held), ROWS(*self._matrix("y_out", y_out, n_rows, cfg[1], u.dtype))))
 
     def aug_scan_backward_batch(self, row_offsets, u, delta, a, b, c, dy, skip=None, z=None, delta_bias=None, softplus: bool = True,
                                 n_group: int = 1, state_in=None, du_out=None, ddelta_out=None, da_out=None, db_out=None, dc_out=None,
                                 dskip_out=None, ddelta_bias_out=None, dz_out=None, row_lengths=None):
-        n_seq, n_rows, _keep, (off, lengths) = self._sequences(row_offsets, row_lengths)
-        if self._check_sizes:
-            check_scan_sizes(n_seq, n_rows, u, delta, a, b, c, n_group,
-                             (("z", z), ("dy", dy), ("du_out", du_out), ("ddelta_out", ddelta_out), ("dz_out", dz_out)),
-                             (("db_out", db_out), ("dc_out", dc_out)), (("state_in", state_in),), da_out,
-                             (("skip", skip), ("delta_bias", delta_bias), ("dskip_out", dskip_out), ("ddelta_bias_out", ddelta_bias_out)))
-        cfg, ins = self._scan_in(u, delta, a, b, c, skip, z, delta_bias, softplus, n_group)
-        m = self._matrix
-        out = ScanGrad(m(du_out), m(ddelta_out), m(db_out), m(dc_out), m(dz_out), self._floats(da_out), self._floats(dskip_out),
-                       self._floats(ddelta_bias_out))
-        self._check(self._lib.aug_scan_backward_batch(self._h, n_seq, off, lengths, cfg, ins, self._floats(state_in), m(dy), out))
+        n_seq, n_rows, _keep, off, lengths = self._sequences(row_offsets, row_lengths)
+        cfg, ins = self._scan_in(n_rows, u, delta, a, b, c, skip, z, delta_bias, softplus, n_group)
+        m, arr, dtype, dim, group = self._matrix, self._array, u.dtype, cfg[1], cfg[2] * n_group
+        out = SCAN_GRAD(
+            *m("du_out", du_out, n_rows, dim, dtype), *m("ddelta_out", ddelta_out, n_rows, dim, dtype),
+            *m("db_out", db_out, n_rows, group, dtype), *m("dc_out", dc_out, n_rows, group, dtype), *m("dz_out", dz_out, n_rows, dim, dtype),
+            arr("da_out", da_out, a.numel()) or 0, arr("dskip_out", dskip_out, dim) or 0, arr("ddelta_bias_out", ddelta_bias_out, dim) or 0)
+        self._check(self._lib.aug_scan_backward_batch(self._h, n_seq, off, lengths, cfg, ins, arr("state_in", state_in, n_seq * a.numel()),
+                                                      ROWS(*m("dy", dy, n_rows, dim, dtype)), out))
 
     def aug_scan_step(self, u, delta, a, b, c, state_in, state_out, y_out, skip=None, z=None, delta_bias=None, softplus: bool = True,
                       n_group: int = 1):
-        n_seq = int(u.shape[0])
-        if self._check_sizes:
-            check_scan_sizes(n_seq, n_seq, u, delta, a, b, c, n_group, (("z", z), ("y_out", y_out)),
-                             states=(("state_in", state_in), ("state_out", state_out)),
-                             per_channel=(("skip", skip), ("delta_bias", delta_bias)))
-        cfg, ins = self._scan_in(u, delta, a, b, c, skip, z, delta_bias, softplus, n_group)
-        self._check(self._lib.aug_scan_step(self._h, n_seq, cfg, ins, self._floats(state_in), self._floats(state_out),
-                                            self._matrix(y_out)))
+        n_seq = u.shape[0]
+        cfg, ins = self._scan_in(n_seq, u, delta, a, b, c, skip, z, delta_bias, softplus, n_group)
+        arr, held = self._array, n_seq * a.numel()
+        self._check(self._lib.aug_scan_step(self._h, n_seq, cfg, ins, arr("state_in", state_in, held), arr("state_out", state_out, held),
+                                            ROWS(*self._matrix("y_out", y_out, n_seq, cfg[1], u.dtype))))

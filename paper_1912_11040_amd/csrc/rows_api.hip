@@ -122,15 +122,15 @@ struct Sequences {
     }
     int64_t end(int i) const { return lengths ? offsets[i] + lengths[i] : offsets[i + 1]; }
 
-    // Cut into blocks of 1 << lg rows.  Memory is found here, nothing is launched.
-    int plan(int lg) {
+    // Cut into blocks of 1 << lg rows, each of which `tiles` work groups share.  Memory is found here, nothing is launched.
+    int plan(int lg, int tiles) {
         aug::RowTables& t = ctx->rows;
         const size_t n = (size_t)n_seq + 1;
         bool same = t.begin.size() == n && !memcmp(t.begin.data(), offsets, n * sizeof(int64_t));
         for (int i = 0; same && i < n_seq; ++i) same = t.end[i] == end(i);
         int64_t items = 0;
         for (int i = 0; i < n_seq; ++i) items += blocks_of(i, lg);
-        if (items >= (int64_t)1 << 24) return fail(ctx, AUG_ERR_UNSUPPORTED, "too many blocks of rows in one call");
+        if (items * tiles >= (int64_t)1 << 24) return fail(ctx, AUG_ERR_UNSUPPORTED, "too many blocks of rows and channels in one call");
         blocks.n_seq = n_seq;
         blocks.lg = lg;
         blocks.n_items = (int)items;
@@ -382,7 +382,7 @@ int aug_short_conv_batch(aug_ctx* ctx, int n_seq, const int64_t* row_offsets, co
         sp.add("y_out", a.y.data, a.y.ld * e, w, seq.n_rows, 1, 0);
         AUG_TRY(sp.check(ctx));
         if (n_seq == 0 || (seq.total == 0 && !state_out)) return AUG_OK;
-        AUG_TRY(seq.plan(aug::short_conv_lg_block(*cfg, false)));
+        AUG_TRY(seq.plan(aug::short_conv_lg_block(*cfg, false), aug::short_conv_tiles(*cfg, false)));
         AUG_TRY(seq.launch());
         a.rows = seq.blocks;
         AUG_TRY(mark(ctx, -1));
@@ -430,7 +430,7 @@ int aug_short_conv_backward_batch(aug_ctx* ctx, int n_seq, const int64_t* row_of
             AUG_HIP(aug::launch_sum_partials(ctx->stream, nullptr, 0, 0, zeros), "gradient sum kernel");
             return AUG_OK;
         }
-        AUG_TRY(seq.plan(aug::short_conv_lg_block(*cfg, true)));
+        AUG_TRY(seq.plan(aug::short_conv_lg_block(*cfg, true), aug::short_conv_tiles(*cfg, true)));
         if (dweight_out || dbias_out) {
             const size_t n = (size_t)aug::short_conv_partials(*cfg, seq.blocks.n_items, ctx->n_cu);
             AUG_TRY(grow(ctx, ctx->seq_ws, 4 * n * cfg->dim * (cfg->taps + 1), "gradient workspace"));
@@ -499,7 +499,7 @@ int aug_scan_batch(aug_ctx* ctx, int n_seq, const int64_t* row_offsets, const in
         sp.add("y_out", a.y.data, a.y.ld * e, cfg->dim * e, seq.n_rows, 1, 0);
         AUG_TRY(sp.check(ctx));
         if (n_seq == 0 || (seq.total == 0 && !state_out)) return AUG_OK;
-        AUG_TRY(seq.plan(aug::scan_lg_block(*cfg, n_seq, row_offsets, row_lengths, ctx->n_cu, false)));
+        AUG_TRY(seq.plan(aug::scan_lg_block(*cfg, n_seq, row_offsets, row_lengths, ctx->n_cu, false), aug::scan_tiles(*cfg, false)));
         seq.abreast = aug::scan_abreast(*cfg, ctx->n_cu);
         if (seq.blocks.lg != aug::kWholeLg) {        // whole sequences need none
             AUG_TRY(grow(ctx, ctx->seq_ws, aug::scan_workspace(*cfg, seq.blocks.n_items, seq.n_rows, ctx->n_cu, false), "scan workspace"));
@@ -553,7 +553,7 @@ int aug_scan_backward_batch(aug_ctx* ctx, int n_seq, const int64_t* row_offsets,
             AUG_HIP(aug::launch_sum_partials(ctx->stream, nullptr, 0, 0, zeros), "gradient sum kernel");
             return AUG_OK;
         }
-        AUG_TRY(seq.plan(aug::scan_lg_block(*cfg, n_seq, row_offsets, row_lengths, ctx->n_cu, true)));
+        AUG_TRY(seq.plan(aug::scan_lg_block(*cfg, n_seq, row_offsets, row_lengths, ctx->n_cu, true), aug::scan_tiles(*cfg, true)));
         AUG_TRY(grow(ctx, ctx->seq_ws, aug::scan_workspace(*cfg, seq.blocks.n_items, seq.n_rows, ctx->n_cu, true), "scan workspace"));
         a.ws = ctx->seq_ws.ptr;
         AUG_TRY(seq.launch());

@@ -97,6 +97,7 @@ struct ScanArgs {
 };
 // Rows of a block as a power of two, kWholeLg: sequences are not cut; of those, how many a row of work groups across the chip takes.
 int scan_lg_block(const aug_scan_cfg& cfg, int n_seq, const int64_t* begin, const int64_t* lengths, int n_cu, bool backward);
+int scan_tiles(const aug_scan_cfg& cfg, bool backward);      // groups of threads across a row
 int scan_abreast(const aug_scan_cfg& cfg, int n_cu);
 size_t scan_workspace(const aug_scan_cfg& cfg, int n_items, int64_t n_rows, int n_cu, bool backward);     // bytes
 hipError_t launch_scan(hipStream_t s, const ScanArgs& a, int n_cu);

@@ -772,8 +772,9 @@ template <class F> hipError_t with_lanes(int n_state, F f) {
     return f(integral_constant<int, 16>(), integral_constant<int, 8>());
 }
 int lanes_of(int n_state) { return n_state <= 4 ? 1 : n_state <= 8 ? 2 : n_state <= 32 ? 4 : n_state <= 64 ? 8 : 16; }
-int scan_tiles(const aug_scan_cfg& cfg) {
-    const int cw = 256 / lanes_of(cfg.n_state);
+int back_lanes_of(int n_state) { return n_state <= 16 ? 4 : n_state <= 64 ? 8 : 16; }
+int scan_tiles(const aug_scan_cfg& cfg, bool backward) {
+    const int cw = 256 / (backward ? back_lanes_of(cfg.n_state) : lanes_of(cfg.n_state));
     return cfg.n_group * ((cfg.dim / cfg.n_group + cw - 1) / cw);
 }
 
@@ -787,7 +788,7 @@ int scan_lg_block(const aug_scan_cfg& cfg, int n_seq, const int64_t* begin, cons
         rows += len;
         longest = longest > len ? longest : len;
     }
-    const int64_t tiles = scan_tiles(cfg), filled = rows * tiles / n_cu;      // rows per compute unit
+    const int64_t tiles = scan_tiles(cfg, false), filled = rows * tiles / n_cu;      // rows per compute unit
     if (longest < 256 || (longest > filled ? longest : filled) < 2 * filled + 128) return kWholeLg;
     int lg = 10;
     while (lg > 6 && (rows >> lg) * tiles < 4 * (int64_t)n_cu) --lg;
@@ -803,15 +804,14 @@ template <class F> hipError_t with_back_lanes(int n_state, F f) {
     return f(integral_constant<int, 16>(), integral_constant<int, 8>());
 }
 BackPlan back_plan(const aug_scan_cfg& cfg, int n_items, int n_cu) {
-    const int cw = 256 / (cfg.n_state <= 16 ? 4 : cfg.n_state <= 64 ? 8 : 16);
     BackPlan p;
-    p.tiles = cfg.n_group * ((cfg.dim / cfg.n_group + cw - 1) / cw);
+    p.tiles = scan_tiles(cfg, true);
     const int64_t runs = (8 * (int64_t)n_cu + p.tiles - 1) / p.tiles;
     p.runs = (int)(runs < n_items ? runs : n_items);
     return p;
 }
 int scan_abreast(const aug_scan_cfg& cfg, int n_cu) {
-    const int n = n_cu / scan_tiles(cfg);
+    const int n = n_cu / scan_tiles(cfg, false);
     return n < 1 ? 1 : n;
 }
 size_t scan_workspace(const aug_scan_cfg& cfg, int n_items, int64_t n_rows, int n_cu, bool backward) {
@@ -821,7 +821,7 @@ size_t scan_workspace(const aug_scan_cfg& cfg, int n_items, int64_t n_rows, int 
 }
 
 hipError_t launch_scan(hipStream_t s, const ScanArgs& a, int n_cu) {
-    const int tiles = scan_tiles(a.cfg);
+    const int tiles = scan_tiles(a.cfg, false);
     return with_type(a.cfg.dtype, [&](auto t) {
         return with_lanes(a.cfg.n_state, [&](auto ln, auto k) {
             return with_full(a.cfg.dim / a.cfg.n_group % (256 / ln.value) == 0, [&](auto full) {
@@ -852,7 +852,7 @@ hipError_t launch_scan(hipStream_t s, const ScanArgs& a, int n_cu) {
 
 hipError_t launch_scan_step(hipStream_t s, int n_seq, const ScanArgs& a, int n_cu) {
     // as many streams to a group as leave eight groups to a compute unit
-    const int64_t tiles = scan_tiles(a.cfg), each = n_seq * tiles / (8 * (int64_t)n_cu);
+    const int64_t tiles = scan_tiles(a.cfg, false), each = n_seq * tiles / (8 * (int64_t)n_cu);
     const int streams = each < 1 ? 1 : each > 16 ? 16 : (int)each;
     return with_type(a.cfg.dtype, [&](auto t) {
         return with_lanes(a.cfg.n_state, [&](auto ln, auto k) {
