@@ -780,8 +780,10 @@ int scan_tiles(const aug_scan_cfg& cfg, bool backward) {
 
 int scan_lg_block(const aug_scan_cfg& cfg, int n_seq, const int64_t* begin, const int64_t* lengths, int n_cu, bool backward) {
     if (backward) return cfg.n_state <= 64 ? 5 : 4;      // BackTile
-    // A row of a group's channels takes some 150 cycles of each of its four SIMDs; a sequence in one piece takes no less than its
-    // length of them.  In blocks the walk is done nearly twice (end states, then outputs), with a launch and the joining between.
+    // Sixteen states: a compute unit with several groups takes some 75 ns for a row of one, a group by itself 136 ns (the latency of its chain), so
+    // that a whole sequence takes no less than its length of those.  In blocks the walk is done nearly twice (end states, then outputs),
+    // some 143 ns a row, with two launches more.  (Four sequences of 4000 rows, 2048 channels: whole 543 us, in blocks 241; 32 of 800, 1024
+    // channels: 143 and 201.)
     int64_t rows = 0, longest = 0;
     for (int i = 0; i < n_seq; ++i) {
         const int64_t len = lengths ? lengths[i] : begin[i + 1] - begin[i];
@@ -789,9 +791,9 @@ int scan_lg_block(const aug_scan_cfg& cfg, int n_seq, const int64_t* begin, cons
         longest = longest > len ? longest : len;
     }
     const int64_t tiles = scan_tiles(cfg, false), filled = rows * tiles / n_cu;      // rows per compute unit
-    if (longest < 256 || (longest > filled ? longest : filled) < 2 * filled + 128) return kWholeLg;
+    if (longest <= filled + 96) return kWholeLg;
     int lg = 10;
-    while (lg > 6 && (rows >> lg) * tiles < 4 * (int64_t)n_cu) --lg;
+    while (lg > 6 && (rows >> lg) * tiles < 8 * (int64_t)n_cu) --lg;
     return lg;
 }
 // The gradients' lanes: at least four per channel, so that a block's elements are eight to a lane at most.
