@@ -11,6 +11,7 @@
 #include <mutex>
 
 #include "api_common.h"
+#include "rows_internal.h"
 
 namespace aug {
 
@@ -534,14 +535,14 @@ int aug_create(aug_ctx** out, int device_id, void* hip_stream) {
         (void)hipGetLastError();
         return AUG_ERR_HIP;
     }
-    aug_ctx* ctx = new (std::nothrow) aug_ctx();
+    aug_ctx* ctx = new (std::nothrow) aug::Context();
     if (!ctx) return AUG_ERR_NOMEM;
     ctx->device = device_id;
     ctx->stream = static_cast<hipStream_t>(hip_stream);
     if (hipDeviceGetAttribute(&ctx->n_cu, hipDeviceAttributeMultiprocessorCount, device_id) != hipSuccess ||
         ctx->n_cu < 1) {
         (void)hipGetLastError();
-        delete ctx;
+        delete &aug::whole(ctx);
         return AUG_ERR_HIP;
     }
     // This device's copy of the static scratch array (once per device, with the device current), and pinned
@@ -552,7 +553,7 @@ int aug_create(aug_ctx** out, int device_id, void* hip_stream) {
             unsigned char* p = nullptr;
             if (hipGetSymbolAddress(reinterpret_cast<void**>(&p), HIP_SYMBOL(scratch)) != hipSuccess || !p) {
                 (void)hipGetLastError();
-                delete ctx;
+                delete &aug::whole(ctx);
                 return AUG_ERR_HIP;
             }
             g_scratch[device_id] = p;
@@ -574,20 +575,21 @@ int aug_destroy(aug_ctx* ctx) {
         (void)hipGetLastError();
         rc = AUG_ERR_HIP;
     }
+    aug::Context& all = aug::whole(ctx);
     DeviceBuffer* bufs[] = {&ctx->d_offsets, &ctx->d_frame_offsets, &ctx->d_conv_items, &ctx->d_conv_first,
                             &ctx->rir_items, &ctx->rir_ctrl, &ctx->visits, &ctx->rir, &ctx->rir_spec, &ctx->reverb, &ctx->energy, &ctx->first_tap, &ctx->vtlp_tab, &ctx->dct, &ctx->mel_tab, &ctx->mel_lanes,
-                            &ctx->window, &ctx->rows.d_begin, &ctx->rows.d_end, &ctx->seq_ws};
+                            &ctx->window, &all.rows.d_begin, &all.rows.d_end, &all.seq_ws};
     for (DeviceBuffer* b : bufs) b->release();
     for (DeviceBuffer& b : ctx->d_frame_items) b.release();
-    for (DeviceBuffer& b : ctx->rows.d_first) b.release();
-    for (DeviceBuffer& b : ctx->rows.d_items) b.release();
+    for (DeviceBuffer& b : all.rows.d_first) b.release();
+    for (DeviceBuffer& b : all.rows.d_items) b.release();
     for (DeviceBuffer& b : ctx->twiddle) b.release();
     for (DeviceBuffer& b : ctx->conv_tab) b.release();
     for (auto& m : ctx->marks) (void)hipEventDestroy(m.first);
     for (hipEvent_t e : ctx->ring.done)
         if (e) (void)hipEventDestroy(e);
     if (ctx->ring.host) (void)hipHostFree(ctx->ring.host);
-    delete ctx;
+    delete &all;
     return rc;
 }
 

@@ -132,18 +132,6 @@ struct MelTableArgs {
     const float* alpha;
     float2* tab;
 };
-
-// The sequences of the last call on feature rows and, per power of two of rows, the table that cuts them into blocks of so many
-// (an empty sequence has one block).  Kept apart from Packing: a step of training alternates between the two.
-struct RowTables {
-    std::vector<int64_t> begin;          // n_seq + 1, as given
-    std::vector<int64_t> end;            // n_seq + 1: end of each sequence (the last entry counts for nothing)
-    static constexpr int kTables = 31;   // blocks of 1 .. 2^30 rows
-    int n_items[kTables] = {};           // blocks; 0: the table is not there
-    DeviceBuffer d_begin, d_end;         // int64 [n_seq+1]
-    DeviceBuffer d_first[kTables];       // int [n_seq+1]: blocks of the sequences before i
-    DeviceBuffer d_items[kTables];       // int2 [n_items]: (sequence, block of it)
-};
 }  // namespace aug
 
 struct aug_ctx {
@@ -185,10 +173,6 @@ struct aug_ctx {
     aug::MelTableArgs mel_args{};        // band edges of the last front-end configuration seen
     bool have_mel_args = false;
     bool have_lanes = false;             // mel_lanes is filled
-
-    // operators on feature rows
-    aug::RowTables rows;
-    aug::DeviceBuffer seq_ws;            // partial sums of gradients; states and sums per stretch of the scan
 
     // stage timing: events recorded in stream order, each tagged with the stage it ends (-1 = a start mark)
     bool profiling = false;

@@ -80,7 +80,7 @@ struct Spans {
 int check_rows(aug_ctx* ctx, const char* name, const aug_rows* m, int64_t n_rows, int64_t width, bool needed) {
     if (!m || !m->data) return needed && n_rows > 0 && width > 0 ? fail(ctx, AUG_ERR_INVALID_ARG, "%s is null", name) : AUG_OK;
     if (m->ld < width) return fail(ctx, AUG_ERR_INVALID_ARG, "ld of %s is less than its width", name);
-    if (m->ld > ((int64_t)1 << 40)) return fail(ctx, AUG_ERR_UNSUPPORTED, "ld of %s is too large", name);
+    if (n_rows > 0 && m->ld > ((int64_t)1 << 48) / n_rows) return fail(ctx, AUG_ERR_UNSUPPORTED, "%s is too large", name);
     return AUG_OK;
 }
 
@@ -124,7 +124,7 @@ struct Sequences {
 
     // Cut into blocks of 1 << lg rows, each of which `tiles` work groups share.  Memory is found here, nothing is launched.
     int plan(int lg, int tiles) {
-        aug::RowTables& t = ctx->rows;
+        aug::RowTables& t = aug::whole(ctx).rows;
         const size_t n = (size_t)n_seq + 1;
         bool same = t.begin.size() == n && !memcmp(t.begin.data(), offsets, n * sizeof(int64_t));
         for (int i = 0; same && i < n_seq; ++i) same = t.end[i] == end(i);
@@ -161,7 +161,7 @@ struct Sequences {
 
     int launch() {
         if (!new_table) return AUG_OK;
-        aug::RowTables& t = ctx->rows;
+        aug::RowTables& t = aug::whole(ctx).rows;
         aug::HostRing& r = ctx->ring;
         const size_t n = (size_t)n_seq + 1, i64 = n * sizeof(int64_t);
         if (new_rows) {
@@ -345,8 +345,8 @@ int aug_rms_norm_backward_batch(aug_ctx* ctx, int64_t n_rows, const aug_norm_cfg
         }
         if (!a.dx.data && !dweight_out) return AUG_OK;
         if (dweight_out) {
-            AUG_TRY(grow(ctx, ctx->seq_ws, 4 * (size_t)aug::norm_partials(n_rows, cfg->dim, ctx->n_cu) * cfg->dim, "gradient workspace"));
-            a.partial = ctx->seq_ws.as<float>();
+            AUG_TRY(grow(ctx, aug::whole(ctx).seq_ws, 4 * (size_t)aug::norm_partials(n_rows, cfg->dim, ctx->n_cu) * cfg->dim, "gradient workspace"));
+            a.partial = aug::whole(ctx).seq_ws.as<float>();
         }
         AUG_TRY(mark(ctx, -1));
         AUG_HIP(aug::launch_norm_backward(ctx->stream, a, ctx->n_cu), "norm gradient kernels");
@@ -433,8 +433,8 @@ int aug_short_conv_backward_batch(aug_ctx* ctx, int n_seq, const int64_t* row_of
         AUG_TRY(seq.plan(aug::short_conv_lg_block(*cfg, true), aug::short_conv_tiles(*cfg, true)));
         if (dweight_out || dbias_out) {
             const size_t n = (size_t)aug::short_conv_partials(*cfg, seq.blocks.n_items, ctx->n_cu);
-            AUG_TRY(grow(ctx, ctx->seq_ws, 4 * n * cfg->dim * (cfg->taps + 1), "gradient workspace"));
-            a.partial = ctx->seq_ws.as<float>();
+            AUG_TRY(grow(ctx, aug::whole(ctx).seq_ws, 4 * n * cfg->dim * (cfg->taps + 1), "gradient workspace"));
+            a.partial = aug::whole(ctx).seq_ws.as<float>();
         }
         AUG_TRY(seq.launch());
         a.rows = seq.blocks;
@@ -502,8 +502,8 @@ int aug_scan_batch(aug_ctx* ctx, int n_seq, const int64_t* row_offsets, const in
         AUG_TRY(seq.plan(aug::scan_lg_block(*cfg, n_seq, row_offsets, row_lengths, ctx->n_cu, false), aug::scan_tiles(*cfg, false)));
         seq.abreast = aug::scan_abreast(*cfg, ctx->n_cu);
         if (seq.blocks.lg != aug::kWholeLg) {        // whole sequences need none
-            AUG_TRY(grow(ctx, ctx->seq_ws, aug::scan_workspace(*cfg, seq.blocks.n_items, seq.n_rows, ctx->n_cu, false), "scan workspace"));
-            a.ws = ctx->seq_ws.ptr;
+            AUG_TRY(grow(ctx, aug::whole(ctx).seq_ws, aug::scan_workspace(*cfg, seq.blocks.n_items, seq.n_rows, ctx->n_cu, false), "scan workspace"));
+            a.ws = aug::whole(ctx).seq_ws.ptr;
         }
         AUG_TRY(seq.launch());
         a.rows = seq.blocks;
@@ -554,8 +554,8 @@ int aug_scan_backward_batch(aug_ctx* ctx, int n_seq, const int64_t* row_offsets,
             return AUG_OK;
         }
         AUG_TRY(seq.plan(aug::scan_lg_block(*cfg, n_seq, row_offsets, row_lengths, ctx->n_cu, true), aug::scan_tiles(*cfg, true)));
-        AUG_TRY(grow(ctx, ctx->seq_ws, aug::scan_workspace(*cfg, seq.blocks.n_items, seq.n_rows, ctx->n_cu, true), "scan workspace"));
-        a.ws = ctx->seq_ws.ptr;
+        AUG_TRY(grow(ctx, aug::whole(ctx).seq_ws, aug::scan_workspace(*cfg, seq.blocks.n_items, seq.n_rows, ctx->n_cu, true), "scan workspace"));
+        a.ws = aug::whole(ctx).seq_ws.ptr;
         AUG_TRY(seq.launch());
         a.rows = seq.blocks;
         AUG_TRY(mark(ctx, -1));

@@ -5,6 +5,25 @@
 
 namespace aug {
 
+// The sequences of the last call on feature rows and, per power of two of rows, the table that cuts them into blocks of so many
+// (an empty sequence has one block).  Kept apart from Packing: a step of training alternates between the two.
+struct RowTables {
+    std::vector<int64_t> begin;          // n_seq + 1, as given
+    std::vector<int64_t> end;            // n_seq + 1: end of each sequence (the last entry counts for nothing)
+    static constexpr int kTables = 31;   // blocks of 1 .. 2^30 rows
+    int n_items[kTables] = {};           // blocks; 0: the table is not there
+    DeviceBuffer d_begin, d_end;         // int64 [n_seq+1]
+    DeviceBuffer d_first[kTables];       // int [n_seq+1]: blocks of the sequences before i
+    DeviceBuffer d_items[kTables];       // int2 [n_items]: (sequence, block of it)
+};
+
+// What aug_create makes: the waveform path's context with the row operators' share of it.
+struct Context : aug_ctx {
+    RowTables rows;
+    DeviceBuffer seq_ws;                 // partial sums of gradients; states and sums per block of the scan
+};
+inline Context& whole(aug_ctx* ctx) { return *static_cast<Context*>(ctx); }
+
 // The sequences of a call, cut into blocks of 1 << lg rows.
 struct RowBlocks {
     int n_seq = 0, lg = 0, n_items = 0;

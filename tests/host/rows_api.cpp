@@ -99,6 +99,9 @@ static void norm(aug_ctx* ctx) {
     REFUSED(AUG_ERR_INVALID_ARG, call(ok, 8, &x, &r, &s, &shifted, nullptr, nullptr));
     REFUSED(AUG_ERR_INVALID_ARG, call(ok, 8, &x, &r, &s, &other, nullptr, nullptr));  // x's place with another ld
     REFUSED(AUG_ERR_INVALID_ARG, call(ok, 8, &x, &r, &s, &narrow, nullptr, nullptr));
+    const aug_rows vast{place(3), (int64_t)1 << 46};
+    REFUSED(AUG_ERR_UNSUPPORTED, call(ok, 8, &x, &r, &s, &vast, nullptr, nullptr));
+    REFUSED(AUG_ERR_UNSUPPORTED, call(ok, (int64_t)1 << 41, &x, &r, &s, &y, nullptr, nullptr));
     const aug_rows left{place(8), 128}, right{place(8) + 128, 128};
     ACCEPTED(call(ok, 8, &left, &r, &s, &right, nullptr, nullptr));    // the two halves of a matrix
     aug_norm_cfg c = ok;
