@@ -703,9 +703,10 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
         sum_rows<G::CW / G::EPT, G::EPT>(par);
 #pragma unroll
         for (int i = 0; i < kept<G::EPT>(); ++i) acc[i] += par[i];
-        for (int e = tid; e < here * 2 * n_state; e += 256) {
-            const int t = e / (2 * n_state), n = e % (2 * n_state), at = n < n_state ? n : n - n_state + G::NP;
-            ws.bc[((int64_t)tile * n_rows + begin + t) * 2 * n_state + n] = (sbc[0][t][at] + sbc[1][t][at]) + (sbc[2][t][at] + sbc[3][t][at]);
+        float* const bc = ws.bc + ((int64_t)tile * n_rows + begin) * 2 * n_state;
+        for (int e = tid; e < here * 2 * G::NP; e += 256) {
+            const int t = e / (2 * G::NP), at = e % (2 * G::NP), n = at % G::NP;
+            if (n < n_state) bc[t * 2 * n_state + (at < G::NP ? n : n_state + n)] = (sbc[0][t][at] + sbc[1][t][at]) + (sbc[2][t][at] + sbc[3][t][at]);
         }
         __syncthreads();
     }
