@@ -248,12 +248,6 @@ def _element_types():
     return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}      # AUG_F32, AUG_BF16, AUG_F16
 
 
-@functools.lru_cache(maxsize=None)
-def _float32():
-    import torch
-    return torch.float32
-
-
 def _element_type(t) -> int:
     try:
         return _element_types()[t.dtype]
@@ -313,6 +307,7 @@ class Augmenter:
         import torch
         self._lib = load_library()
         self._check_sizes = bool(check_sizes)
+        self._f32 = torch.float32
         if stream is None:
             stream = torch.cuda.current_stream(device)
         self.stream = stream
@@ -471,17 +466,27 @@ class Augmenter:
             raise ValueError(f"{name} is on {t.device}, the context on device {self.device}")
         return t.data_ptr()
 
+    # (the common case is settled in one expression: a step of a few streams takes the GPU less time than its arguments take here)
+
     def _matrix(self, name, t, n_rows, width, dtype):
         """The fields of aug_rows (None: no matrix)."""
         if t is None:
             return 0, 0
+        if t.shape == (n_rows, width) and t.dtype is dtype and t.get_device() == self.device:
+            down, across = t.stride()
+            if across == 1 and down >= width:
+                return t.data_ptr(), down
         ld = check_matrix(name, t, n_rows, width, dtype)
         return self._on_device(name, t), ld
 
     def _array(self, name, t, count, dtype=None):
         if t is None:
             return None
-        check_array(name, t, count, _float32() if dtype is None else dtype)
+        if dtype is None:
+            dtype = self._f32
+        if t.numel() == count and t.dtype is dtype and t.is_contiguous() and t.get_device() == self.device:
+            return t.data_ptr()
+        check_array(name, t, count, dtype)
         return self._on_device(name, t)
 
     @staticmethod

@@ -57,7 +57,7 @@ def host():
     if not os.path.exists(B.LIB_PATH):
         build.build()
     a = B.Augmenter.__new__(B.Augmenter)
-    a._lib, a._check_sizes, a.device, a._h = B.load_library(), True, -1, None
+    a._lib, a._check_sizes, a._f32, a.device, a._h = B.load_library(), True, torch.float32, -1, None
     return a
 
 
