@@ -25,26 +25,28 @@ __global__ __launch_bounds__(256) void row_tables_kernel(RowTableArgs a) {
     for (int j = l; j < a.first[i + 1] - from; j += lanes) a.items[from + j] = make_int2(i, j);
 }
 
-// 64 columns to a group, every fourth row a wavefront's, eight rows' loads on their way at once (one row after another took 38 us for
-// 128 rows).
-constexpr int kColumns = 64;
-__global__ __launch_bounds__(4 * kColumns) void sum_partials_kernel(const float* partial, int n_partial, int64_t stride, SumOuts outs) {
-    __shared__ float part[4][kColumns];
-    const int lane = threadIdx.x % kColumns, wave = threadIdx.x / kColumns;
+// Sixteen columns to a group, every sixteenth row a lane's, eight rows' loads on their way at once: few columns of many rows are bound by
+// latency (512 rows of 1001: 64 columns and four rows side by side took 12 us, so 5; one row after another 38 for 128 rows).
+constexpr int kColumns = 16, kAbreast = 16;
+__global__ __launch_bounds__(kColumns * kAbreast) void sum_partials_kernel(const float* partial, int n_partial, int64_t stride, SumOuts outs) {
+    __shared__ float part[kAbreast][kColumns];
+    const int lane = threadIdx.x % kColumns, group = threadIdx.x / kColumns;
     const int64_t c = (int64_t)blockIdx.x * kColumns + lane, width = outs.part[0].width + outs.part[1].width + outs.part[2].width;
     constexpr int kAhead = 8;
     float acc = 0.f;
-    for (int p = wave; p < n_partial; p += 4 * kAhead) {
+    for (int p = group; p < n_partial; p += kAbreast * kAhead) {
         float v[kAhead];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) v[j] = c < width && p + 4 * j < n_partial ? partial[(p + 4 * j) * stride + c] : 0.f;
+        for (int j = 0; j < kAhead; ++j) v[j] = c < width && p + kAbreast * j < n_partial ? partial[(int64_t)(p + kAbreast * j) * stride + c] : 0.f;
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) acc += v[j];
     }
-    part[wave][lane] = acc;
+    part[group][lane] = acc;
     __syncthreads();
-    if (wave || c >= width) return;
-    const float sum = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
+    if (group || c >= width) return;
+    float sum = 0.f;
+#pragma unroll
+    for (int g = 0; g < kAbreast; ++g) sum += part[g][lane];
     int64_t at = c;
     for (const SumOuts::Out& o : outs.part) {
         if (at >= 0 && at < o.width && o.out) o.out[at] = sum;
@@ -63,7 +65,7 @@ hipError_t launch_row_tables(hipStream_t s, const RowTableArgs& a) {
 hipError_t launch_sum_partials(hipStream_t s, const float* partial, int n_partial, int64_t stride, const SumOuts& outs) {
     const int64_t width = outs.part[0].width + outs.part[1].width + outs.part[2].width;
     if (width <= 0) return hipSuccess;
-    sum_partials_kernel<<<dim3((unsigned)((width + kColumns - 1) / kColumns)), dim3(4 * kColumns), 0, s>>>(partial, n_partial, stride, outs);
+    sum_partials_kernel<<<dim3((unsigned)((width + kColumns - 1) / kColumns)), dim3(kColumns * kAbreast), 0, s>>>(partial, n_partial, stride, outs);
     return hipGetLastError();
 }
 
