@@ -34,6 +34,8 @@
  *     response, window or cepstrum length (which may move or rewrite the
  *     workspace), before front-end calls with more than 15 other combinations
  *     of hop, feature, channels and mixture on the fly, and before aug_destroy.
+ *     (The sequences of the operators on feature rows are kept apart from the utterances of the other calls: "other
+ *     offsets" means other ones of the same kind.)
  *     A call that would have to allocate, copy offsets or rebuild tables while
  *     its stream is being captured returns AUG_ERR_UNSUPPORTED instead.
  *   - Every function returns AUG_OK (0) or a negative aug_status; nothing is

@@ -208,13 +208,13 @@ struct RowShape {
     int lanes, vecs, groups;
 };
 // Forward: a row's whole width to a group where it takes one, so that many wavefronts have loads on their way (64 utterances at 2048
-// columns 183 us with a wavefront per row; 32 groups a compute unit 153, 16 162, 8 as many as 183: the last round is half empty).
+// columns into 8 bits 198 us with a wavefront per row; 32 groups a compute unit 149, 16 162, 8 183: the last round is half empty).
 constexpr RowShape forward_shape(int dim) {
     return dim <= 128 ? RowShape{16, 1, 16} : dim <= 512 ? RowShape{64, 1, 16} : dim <= 2048 ? RowShape{256, 1, 32}
          : dim <= 4096 ? RowShape{512, 1, 8} : dim <= 8192 ? RowShape{1024, 1, 4} : RowShape{1024, 2, 4};
 }
-// Gradients: each group leaves a row of sums, so few groups with much on their way each (20011 rows of 1001 columns: two groups a
-// compute unit 72 us, four 84; a group per row 82.  20000 of 2048: 86, with a wavefront per row 106).
+// Gradients: each group leaves a row of sums, so few groups with much on their way each (20011 rows of 1001 columns: 69 us, with four groups a
+// compute unit 12 more, with a group per row 10.  20000 of 2048: 85, with a wavefront per row 106).
 constexpr RowShape backward_shape(int dim) {
     return dim <= 128 ? RowShape{16, 1, 4} : dim <= 512 ? RowShape{64, 1, 4} : dim <= 1024 ? RowShape{64, 2, 2} : dim <= 2048 ? RowShape{256, 1, 4}
          : dim <= 4096 ? RowShape{512, 1, 2} : dim <= 8192 ? RowShape{1024, 1, 1} : RowShape{1024, 2, 1};

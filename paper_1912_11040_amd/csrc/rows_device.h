@@ -42,7 +42,8 @@ template <class T, int N> __device__ inline void store_pack(T* p, const Pack<T, 
         if (i < valid) p[i] = r.v[i];
 }
 
-// A stretch of channels of row r.  FULL: all of it is there, one access without a branch; else `valid` elements of it.
+// A stretch of channels of row r.  FULL: all of it is there, one access without a branch; else `valid` elements of it.  (With a branch per
+// load the loads of several rows wait for one another where the branches meet: the short convolution of 64 utterances 157 us, so 95.)
 template <class T, int VE, bool FULL> __device__ inline Pack<T, VE> load_part(const aug_rows& m, int64_t r, int col, int valid) {
     if constexpr (FULL) {
         Pack<T, VE> v;
