@@ -297,3 +297,109 @@ def test_matrices_beyond_2_to_31_elements():
                 for i, (p, q) in enumerate(zip(first, kept)):
                     assert torch.equal(p, q), i
             first = kept
+
+
+def test_two_contexts_on_two_streams():
+    """The same work at once in two contexts, each on a stream of its own, against one alone."""
+    off = np.array([0, 300, 301, 900])
+    rows, blk = 900, Block(torch.float32, 11)
+    with binding.Augmenter(0) as aug:
+        want = blk.buffers(rows, 3)
+        want["x"].normal_()
+        want["made"].normal_()
+        dy = torch.randn(rows, DIM, device="cuda")
+
+        def work(a, b):
+            a.aug_rms_norm_batch(b["x"], blk.norm_w, sum_out=b["sum"], y_out=b["norm"], rstd_out=b["rstd"])
+            a.aug_short_conv_batch(off, b["norm"], blk.conv_w, b["conv"], bias=blk.conv_b, state_out=b["conv_state"])
+            a.aug_scan_batch(off, **blk.scan_args(b), y_out=b["y"], state_out=b["state"])
+            blk.backward(a, b, off, dy)
+
+        work(aug, want)
+    sides = []
+    for _ in range(2):
+        b = blk.buffers(rows, 3)
+        b["x"].copy_(want["x"])
+        b["made"].copy_(want["made"])
+        stream = torch.cuda.Stream()
+        sides.append((stream, binding.Augmenter(0, stream), b))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for stream, a, b in sides:
+            work(a, b)
+    torch.cuda.synchronize()
+    for _, a, b in sides:
+        a.close()
+        for n in want:
+            assert torch.equal(b[n].nan_to_num(), want[n].nan_to_num()), n
+
+
+def test_as_many_sequences_as_there_may_be():
+    """65535 sequences of one row or none, against the formulas of a single row."""
+    n_seq, dim, n = 65535, 9, 3
+    lengths = (np.arange(n_seq) % 5 != 2).astype(np.int64)
+    off = np.concatenate([[0], np.cumsum(lengths)])
+    rows, r = int(off[-1]), lambda *s: torch.randn(*s, device="cuda")          # noqa: E731
+    x, delta, b, c, dy, w = r(rows, dim), r(rows, dim), r(rows, n), r(rows, n), r(rows, dim), r(dim, 4)
+    a, state, cstate = -torch.rand(dim, n, device="cuda"), r(n_seq, dim, n), r(n_seq, 3, dim)
+    y, yc, du, dxc = (torch.empty_like(x) for _ in range(4))
+    out, cout, da = torch.empty_like(state), torch.empty_like(cstate), torch.empty_like(a)
+    with binding.Augmenter(0) as aug:
+        aug.aug_scan_batch(off, x, delta, a, b, c, y, state_in=state, state_out=out)
+        aug.aug_scan_backward_batch(off, x, delta, a, b, c, dy, state_in=state, du_out=du, da_out=da)
+        aug.aug_short_conv_batch(off, x, w, yc, activation="none", state_in=cstate, state_out=cout)
+        aug.aug_short_conv_backward_batch(off, x, w, dy, activation="none", state_in=cstate, dx_out=dxc)
+        torch.cuda.synchronize()
+    has = torch.from_numpy(lengths > 0).cuda()
+    f = lambda t: t.double()          # noqa: E731
+    step, h0 = torch.nn.functional.softplus(f(delta)), f(state)[has]
+    e = torch.exp(step[:, :, None] * f(a))
+    h = e * h0 + (step * f(x))[:, :, None] * f(b)[:, None]
+    g = f(dy)[:, :, None] * f(c)[:, None]
+
+    def close(got, want, mag):          # 80 roundings of the terms' magnitudes
+        assert bool(((f(got) - want).abs() <= 80 * 2.0 ** -24 * mag).all())
+
+    mag = e * h0.abs() + (step * f(x).abs())[:, :, None] * f(b).abs()[:, None]
+    close(out[has], h, mag)
+    assert torch.equal(out[~has], state[~has]) and torch.equal(cout[~has], cstate[~has])
+    close(y, (h * f(c)[:, None]).sum(2), (mag * f(c).abs()[:, None]).sum(2))
+    close(du, step * (g * f(b)[:, None]).sum(2), step * (g * f(b)[:, None]).abs().sum(2))
+    terms = g * e * h0 * step[:, :, None]
+    assert bool(((f(da) - terms.sum(0)).abs() <= (80 + 2048) * 2.0 ** -24 * terms.abs().sum(0)).all())      # as many blocks in a run, at most
+    p = torch.cat([f(cstate)[has], f(x)[:, None]], 1) * f(w).t()
+    close(yc, p.sum(1), p.abs().sum(1))
+    assert torch.equal(cout[has], torch.cat([cstate[has][:, 1:], x[:, None]], 1))
+    close(dxc, f(dy) * f(w)[:, 3], (f(dy) * f(w)[:, 3]).abs())
+
+
+@pytest.mark.parametrize("dim,n,g", [(32768, 2, 1), (32768, 2, 4096), (8192, 128, 2)])
+def test_as_many_channels_as_there_may_be(dim, n, g):
+    off, rows = np.array([0, 2, 2, 5]), 5
+    r = np.random.default_rng(12)
+    t = {k: dev(r.standard_normal((rows, w)).astype(np.float32)).bfloat16() for k, w in dict(u=dim, delta=dim, b=g * n, c=g * n).items()}
+    t["a"] = dev(-np.exp(r.uniform(-2, 1, (dim, n))).astype(np.float32))
+    dy, w = dev(r.standard_normal((rows, dim)).astype(np.float32)).bfloat16(), dev(r.standard_normal((dim, 3)).astype(np.float32))
+    y, yc, dx = (torch.empty_like(dy) for _ in range(3))
+    state = torch.empty(3, dim, n, device="cuda")
+    grads = dict(du=torch.empty_like(dy), ddelta=torch.empty_like(dy), db=torch.empty_like(t["b"]), dc=torch.empty_like(t["c"]),
+                 da=torch.empty_like(t["a"]))
+    dw = torch.empty_like(w)
+    with binding.Augmenter(0) as aug:
+        aug.aug_scan_batch(off, **t, y_out=y, n_group=g, state_out=state)
+        aug.aug_scan_backward_batch(off, **t, dy=dy, n_group=g, **{k + "_out": v for k, v in grads.items()})
+        aug.aug_short_conv_batch(off, t["u"], w, yc)
+        aug.aug_short_conv_backward_batch(off, t["u"], w, dy, dx_out=dx, dweight_out=dw)
+        torch.cuda.synchronize()
+    ws = {k: wide(v) for k, v in t.items()}
+    want, mag = R.scan(off, n_group=g, **ws), R.scan(off, n_group=g, magnitude=True, **ws)
+    near(y, want[0], mag[0], 64 + 6 * 3 + n, "y")
+    near(state, want[1], mag[1], 64 + 6 * 3 + n, "state")
+    want, mag = (R.scan_backward(off, n_group=g, dy=wide(dy), magnitude=m, **ws) for m in (False, True))
+    for k, v in grads.items():
+        near(v, want[k], mag[k], 2 * (64 + 6 * 3 + n) + (dim // g if k in ("db", "dc") else rows), k)
+    args = (off, wide(t["u"]), wide(w))
+    near(yc, R.short_conv(*args)[0], R.short_conv(*args, magnitude=True)[0], 3 + 12, "conv")
+    want, mag = R.short_conv_backward(*args, wide(dy)), R.short_conv_backward(*args, wide(dy), magnitude=True)
+    near(dx, want[0], mag[0], 6 + 16, "dx")
+    near(dw, want[1], mag[1], 3 + 16 + rows, "dw")
