@@ -104,12 +104,12 @@ constexpr float kLog2e = 1.44269504088896341f;
 // exp(x) by the hardware's power of two, whose argument's rounding is 2^-24 |x log2 e| of the result.
 __device__ inline float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 __device__ inline float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + exp_fast(-x)); }      // 0 and 1 at the infinities
-// ln(1 + exp(x)) = max(x, 0) + ln(1 + e), e = exp(-|x|).  With w = 1 + e rounded, ln(w) e / (w - 1) has the relative accuracy
-// of ln: the rounding of w is in both (for e below half a step of 1, w is 1 and the value e).
+// ln(1 + exp(x)) = max(x, 0) + ln(1 + e), e = exp(-|x|).  With w = 1 + e rounded and r = e - (w - 1), which is exact, ln(1 + e) =
+// ln(w) + ln(1 + r / w); r is at most 2^-24, so that r alone is off by r e / w, 2^-24 of the value.  (For e below half a step of 1, w is 1
+// and the value e.)
 __device__ inline float softplus(float x) {
-    const float e = exp_fast(-fabsf(x)), w = 1.f + e, d = w - 1.f;
-    const float l = d == 0.f ? e : __builtin_amdgcn_logf(w) * 0.693147180559945309f * (e * __builtin_amdgcn_rcpf(d));
-    return fmaxf(x, 0.f) + l;      // (a NaN is in l, whatever fmaxf drops)
+    const float e = exp_fast(-fabsf(x)), w = 1.f + e;
+    return fmaxf(x, 0.f) + fmaf(__builtin_amdgcn_logf(w), 0.693147180559945309f, e - (w - 1.f));      // (a NaN is in e, whatever fmaxf drops)
 }
 
 }  // namespace aug
