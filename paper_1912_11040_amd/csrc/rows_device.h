@@ -78,6 +78,16 @@ template <int LN> __device__ inline float lanes_sum(float v) {
     }
     return v;
 }
+// Four sums over the lanes of a quad, lane q of it gets the q-th: halved twice by the bits of q, nine instructions where four sums and
+// their selection take twelve.
+__device__ inline float quad_sums(const float (&v)[4]) {
+    const bool odd = threadIdx.x & 1, high = threadIdx.x & 2;
+    auto pass = [](float x, auto ctrl) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), ctrl.value, 0xf, 0xf, true)); };
+    const std::integral_constant<int, 0xB1> next;
+    const std::integral_constant<int, 0x4E> second;
+    const float low = (odd ? v[1] : v[0]) + pass(odd ? v[0] : v[1], next), up = (odd ? v[3] : v[2]) + pass(odd ? v[2] : v[3], next);
+    return (high ? up : low) + pass(high ? low : up, second);
+}
 // The largest of so many neighbouring lanes' values likewise; `lanes` is the same for the whole wavefront.
 template <int CTRL> __device__ inline unsigned dpp_max(unsigned v) {
     const unsigned o = __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true);

@@ -134,15 +134,16 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int all_tiles, fl
         constexpr int kTogether = LN < 4 ? 4 : LN;
         int t = 0;
         for (; t + kTogether <= here; t += kTogether) {
-            float y = 0.f;
+            float y = 0.f, p[kTogether];
 #pragma unroll
             for (int j = 0; j < kTogether; ++j) {
-                const float p = walk(t + j);
-                if (MODE == kSums) continue;
-                const float all = lanes_sum<LN>(p);      // lane q of a channel keeps row q of LN
+                p[j] = walk(t + j);
+                if (MODE == kSums || LN == 4) continue;
+                const float all = lanes_sum<LN>(p[j]);   // lane q of a channel keeps row q of LN
                 y = j % LN == 0 || j % LN == tid % LN ? all : y;
                 if (j % LN == LN - 1) sy[t + j - (LN - 1) + tid % LN][ch] = y;
             }
+            if constexpr (MODE != kSums && LN == 4) sy[t + tid % LN][ch] = quad_sums(p);
         }
         for (; t < here; ++t) {
             const float p = walk(t);
@@ -610,7 +611,7 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
                     h[j + 1][k] = fmaf(e[j][k], h[j][k], x.s.y * x.v[k]);
                 }
             }
-            float keep_gb = 0.f, keep_eh = 0.f, keep_p = 0.f;
+            float of_gb[4] = {}, of_eh[4] = {}, of_p[4] = {};
             RowIn<K> next_c;
             next.load(su, sdp, sb, (s + 1) * G::SUB - 1, ch, nq);
             next_c.load(su, sdp, sc, (s + 1) * G::SUB - 1, ch, nq);
@@ -636,18 +637,28 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
                     w[k] = g * x.s.y;
                     w[K + k] = x.dp * h[j + 1][k];
                 }
-                gb = lanes_sum<LN>(gb);
-                eha = lanes_sum<LN>(eha);
-                p = lanes_sum<LN>(p);
                 // lane q of a channel keeps every LN-th row; the rows' steps are not read again
                 constexpr int kTurns = LN < G::SUB ? LN : G::SUB;
-                const bool mine = j % kTurns == tid % LN;
-                keep_gb = mine ? gb : keep_gb;
-                keep_eh = mine ? eha : keep_eh;
-                keep_p = mine ? p : keep_p;
-                if (j % kTurns == 0 && tid % LN < kTurns) {
-                    su[t + tid % LN][ch] = make_float2(keep_gb, keep_eh);
-                    sdp[t + tid % LN][ch] = keep_p;
+                if constexpr (LN == 4) {
+                    of_gb[j % 4] = gb;
+                    of_eh[j % 4] = eha;
+                    of_p[j % 4] = p;
+                    if (j % 4 == 0) {
+                        su[t + tid % LN][ch] = make_float2(quad_sums(of_gb), quad_sums(of_eh));
+                        sdp[t + tid % LN][ch] = quad_sums(of_p);
+                    }
+                } else {
+                    gb = lanes_sum<LN>(gb);
+                    eha = lanes_sum<LN>(eha);
+                    p = lanes_sum<LN>(p);
+                    const bool mine = j % kTurns == tid % LN;
+                    of_gb[0] = mine ? gb : of_gb[0];
+                    of_eh[0] = mine ? eha : of_eh[0];
+                    of_p[0] = mine ? p : of_p[0];
+                    if (j % kTurns == 0 && tid % LN < kTurns) {
+                        su[t + tid % LN][ch] = make_float2(of_gb[0], of_eh[0]);
+                        sdp[t + tid % LN][ch] = of_p[0];
+                    }
                 }
                 // sums over the wavefront's channels (bits log2 LN .. 5 of the lane): a quarter of the values to each 16 lanes
                 halve<5, V>(w);
