@@ -28,7 +28,7 @@ __device__ inline float rate2(float a) {
 //
 //   h = exp(step a) h + step u b,   y = (sum c h + skip u) z sigmoid(z)
 // A state's row is a product, an exponential (four issue slots), a product and two multiply-adds: at sixteen states 128 slots a
-// (row, channel) against 8 bytes of 16-bit rows, so vector issue bounds it (64 utterances of 98 to 1598 rows, 1024 channels, bf16: 251 us, 86 % of
+// (row, channel) against 8 bytes of 16-bit rows, so vector issue bounds it (64 utterances of 98 to 1598 rows, 1024 channels, bf16: 249 us, 86 % of
 // the slots busy; their bytes would take 97 us at the rate of a copy).
 // A group of four wavefronts takes 256 / LN channels through a block of rows; LN neighbouring lanes share a channel, K states each
 // in registers, and add up their part of the output.  (A lane per channel would need no sums and a quarter of the groups; the chip is
@@ -299,8 +299,8 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, int n_seq, i
 // the block's share of e_first g_first, which is what it hands to the rows before it.  scan_back_join_kernel then makes of F the state
 // before each block and of R what comes in from behind.  With both the blocks are independent of one another: the main pass
 // walks a block forward for its states and back for its gradients, in stretches of SUB rows whose states and decays stay in registers.
-// Both are bound by vector issue: 32 utterances of 98 to 1598 rows, 1024 channels, 16 states, bf16 take 165 us (80 % of the slots) and 480 (76 %),
-// the join between them 49 (HBM), 677 in all.  In blocks of 32 rows the sums are 8 of the 30 bytes moved a (row, channel); stretches of 16
+// Both are bound by vector issue: 32 utterances of 98 to 1598 rows, 1024 channels, 16 states, bf16 take 165 us (80 % of the slots) and 473 (76 %),
+// the join between them 49 (HBM), 670 in all.  In blocks of 32 rows the sums are 8 of the 30 bytes moved a (row, channel); stretches of 16
 // rows need more registers than two wavefronts per SIMD leave (1250 us with one).
 template <int LN, int K> struct BackTile {
     static constexpr int CW = 256 / LN, NP = LN * K, LG = NP <= 64 ? 5 : 4, RT = 1 << LG, EPT = RT * CW / 256, SUB = K <= 2 ? 16 : 8;
