@@ -39,9 +39,12 @@ template <int LN, int K> struct Tile {
     static constexpr int BC = (TT * NP + 255) / 256;     // elements of b (and of c) that a lane fetches per tile
 };
 
+// SPARE: some lanes have states that the channel does not have (n_state is less than LN K).  Their b and c are zero, and they are put
+// to zero after every row: a step, an input or a gradient that is infinite or NaN would make NaN of them, and of the sums that they are in.
+
 enum ScanMode { kWhole, kSums, kResume };                // the block is a sequence; its end state from zero and its steps' sum; from its first state
 
-template <class T, int LN, int K, int MODE, bool FULL>
+template <class T, int LN, int K, int MODE, bool FULL, bool SPARE>
 __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int all_tiles, float* first_state, float* step_sum) {
     using G = Tile<LN, K>;
     __shared__ float2 su[G::TT][G::CW];                  // (step, step u)
@@ -126,6 +129,7 @@ __global__ __launch_bounds__(256) void scan_kernel(ScanArgs a, int all_tiles, fl
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 h[k] = fmaf(__builtin_amdgcn_exp2f(s.x * rate[k]), h[k], s.y * sb[t][nq + k]);
+                if (SPARE && nq + k >= n_state) h[k] = 0.f;
                 if (MODE != kSums) p = fmaf(sc[t][nq + k], h[k], p);
             }
             if (MODE == kSums) sum += s.x;
@@ -456,7 +460,7 @@ template <int K> struct RowIn {
 };
 __device__ inline void stay_ahead() { __builtin_amdgcn_sched_barrier(0x2 | 0x4 | 0x200); }      // arithmetic and LDS writes may pass, reads not
 
-template <class T, int LN, int K, bool FULL>
+template <class T, int LN, int K, bool FULL, bool SPARE>
 __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs a, BackWs ws, BackPlan plan, int64_t n_rows, bool joined) {
     using G = BackTile<LN, K>;
     constexpr int NS = G::RT / G::SUB, V = 2 * K;
@@ -589,7 +593,7 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
                     for (int k = 0; k < K; ++k) st[k] = fmaf(__builtin_amdgcn_exp2f(x.x * rate[k]), st[k], x.y * sb[t][nq + k]);
                 }
 #pragma unroll
-                for (int k = 0; k < K; ++k) sst[s][tid][k] = st[k];
+                for (int k = 0; k < K; ++k) sst[s][tid][k] = SPARE && nq + k >= n_state ? 0.f : st[k];
             }
         }
         // (rows behind the sequence's end inside a stretch have steps and dp of zero)
@@ -609,6 +613,7 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
                 for (int k = 0; k < K; ++k) {
                     e[j][k] = __builtin_amdgcn_exp2f(x.s.x * rate[k]);
                     h[j + 1][k] = fmaf(e[j][k], h[j][k], x.s.y * x.v[k]);
+                    if (SPARE && nq + k >= n_state) e[j][k] = h[j + 1][k] = 0.f;
                 }
             }
             float of_gb[4] = {}, of_eh[4] = {}, of_p[4] = {};
@@ -627,7 +632,9 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
                 float gb = 0.f, eha = 0.f, p = 0.f, w[V];
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
-                    const float c = xc.v[k], g = fmaf(c, x.dp, carried[k]);
+                    const float c = xc.v[k];
+                    float g = fmaf(c, x.dp, carried[k]);
+                    if (SPARE && nq + k >= n_state) g = 0.f;
                     carried[k] = e[j][k] * g;
                     const float eh = carried[k] * h[j][k];
                     p = fmaf(c, h[j + 1][k], p);
@@ -783,6 +790,9 @@ template <class F> void with_groups(bool eight, F f) {
     else f(std::integral_constant<int, 1>());
 }
 
+// Calls f with whether lanes have states to spare.
+template <class F> hipError_t with_spare(bool spare, F f) { return spare ? f(std::true_type()) : f(std::false_type()); }
+
 // Calls f with the lanes per channel and the states per lane for so many states, as integral constants.
 template <class F> hipError_t with_lanes(int n_state, F f) {
     using std::integral_constant;
@@ -854,10 +864,12 @@ hipError_t launch_scan(hipStream_t s, const ScanArgs& a, int n_cu) {
                 float* const first_state = static_cast<float*>(a.ws);
                 float* const step_sum = first_state + (int64_t)a.rows.n_items * a.cfg.dim * a.cfg.n_state;
                 if (a.rows.lg == kWholeLg) {
-                    scan_kernel<T, ln.value, k.value, kWhole, full.value><<<grid, dim3(256), 0, s>>>(a, tiles, nullptr, nullptr);
-                    return hipGetLastError();
+                    return with_spare(a.cfg.n_state < ln.value * k.value, [&](auto spare) {
+                        scan_kernel<T, ln.value, k.value, kWhole, full.value, spare.value><<<grid, dim3(256), 0, s>>>(a, tiles, nullptr, nullptr);
+                        return hipGetLastError();
+                    });
                 }
-                scan_kernel<T, ln.value, k.value, kSums, full.value><<<grid, dim3(256), 0, s>>>(a, tiles, first_state, step_sum);
+                scan_kernel<T, ln.value, k.value, kSums, full.value, false><<<grid, dim3(256), 0, s>>>(a, tiles, first_state, step_sum);
                 hipError_t e = hipGetLastError();
                 if (e != hipSuccess) return e;
                 const int64_t width = (int64_t)a.cfg.dim * a.cfg.n_state;
@@ -867,8 +879,10 @@ hipError_t launch_scan(hipStream_t s, const ScanArgs& a, int n_cu) {
                 });
                 e = hipGetLastError();
                 if (e != hipSuccess) return e;
-                scan_kernel<T, ln.value, k.value, kResume, full.value><<<grid, dim3(256), 0, s>>>(a, tiles, first_state, step_sum);
-                return hipGetLastError();
+                return with_spare(a.cfg.n_state < ln.value * k.value, [&](auto spare) {
+                    scan_kernel<T, ln.value, k.value, kResume, full.value, spare.value><<<grid, dim3(256), 0, s>>>(a, tiles, first_state, step_sum);
+                    return hipGetLastError();
+                });
             });
         });
     });
@@ -908,8 +922,10 @@ hipError_t launch_scan_backward(hipStream_t s, const ScanArgs& a, int64_t n_rows
                     e = hipGetLastError();
                     if (e != hipSuccess) return e;
                 }
-                scan_back_kernel<T, ln.value, k.value, full.value><<<dim3((unsigned)(plan.tiles * plan.runs)), dim3(256), 0, s>>>(a, ws, plan, n_rows, joined);
-                return hipGetLastError();
+                return with_spare(a.cfg.n_state < ln.value * k.value, [&](auto spare) {
+                    scan_back_kernel<T, ln.value, k.value, full.value, spare.value><<<dim3((unsigned)(plan.tiles * plan.runs)), dim3(256), 0, s>>>(a, ws, plan, n_rows, joined);
+                    return hipGetLastError();
+                });
             });
             if (e != hipSuccess || (!a.grad.db.data && !a.grad.dc.data)) return e;
             scan_bc_kernel<T><<<dim3((unsigned)a.rows.n_items), dim3(256), 0, s>>>(a, ws, plan, n_rows);

@@ -1,0 +1,96 @@
+"""The operators on feature rows where 32 bits end: infinite steps, inputs that are no numbers, growing states, rows beyond the range of their
+squares.  What the definition keeps finite stays finite, and what it makes infinite is infinite."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import rows_oracle as R
+from paper_1912_11040_amd import binding
+from tests import test_gpu_scan as S
+from tests.rows_parity import TYPES, half_step, wide
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def aug():
+    with binding.Augmenter(0) as a:
+        yield a
+
+
+def agrees(got, want, mag, terms, name):
+    """got is want to within its rounding where want is finite, the same infinity where it is one, and no number where it is none."""
+    g = wide(got).reshape(want.shape)
+    finite = np.isfinite(want)
+    assert np.isfinite(mag[finite]).all(), f"{name}: the bound says nothing"
+    tol = half_step(got.dtype) * np.abs(want) * (1 + 2.0 ** -7) + terms * 2.0 ** -24 * mag + (2.0 ** -25 if got.dtype == torch.float16 else 0)
+    with np.errstate(invalid="ignore"):
+        bad = np.where(finite, ~(np.abs(g - want) <= tol), np.where(np.isnan(want), np.isfinite(g), g != want))
+    assert not bad.any(), f"{name}: {bad.sum()} of {bad.size} off, first at {tuple(np.argwhere(bad)[0])}: {g[bad][0]!r} for {want[bad][0]!r}"
+
+
+def _gradients(aug, off, t, dy, g, state, softplus=True):
+    like = dict(du="u", ddelta="delta", db="b", dc="c", dz="z")
+    out = {k: torch.full(t[v].shape, 7.0, dtype=dy.dtype, device="cuda") for k, v in like.items() if v in t}
+    out.update(da=torch.empty_like(t["a"]), dskip=torch.empty_like(t["a"][:, 0]), ddelta_bias=torch.empty_like(t["a"][:, 0]))
+    aug.aug_scan_backward_batch(off, **t, dy=dy, n_group=g, softplus=softplus, state_in=state, **{k + "_out": v for k, v in out.items()})
+    return out
+
+
+# ---- a step that is infinite: the state forgets, and the gradient stops there ----
+
+@pytest.mark.parametrize("name", ["f16", "f32"])
+@pytest.mark.parametrize("n", [1, 2, 3, 5, 7, 8, 11, 16, 17, 33, 65, 100, 128])
+@pytest.mark.parametrize("lengths,last", [([21, 13, 4], True), ([30, 300, 9], False)])
+def test_infinite_step(aug, lengths, last, n, name):
+    """One channel's step is infinite in one row of the second sequence.  The rows before it (their gradients too), the other channels and the
+    other sequences are those of the definition, whatever the number of states; in that row the output is infinite."""
+    dim, g, d = 70, 2, 41
+    off, _, t, state, dy = S._inputs(lengths, dim, n, g, TYPES[name], 300 + n)
+    at = int(off[2]) - 1 if last else int(off[1]) + lengths[1] // 2
+    t["delta"][at, d] = float("inf")
+    for k in ("u", "b", "c", "z"):                        # one sign, so that the definition's output there is an infinity
+        t[k][at] = t[k][at].abs() + 0.125
+    args = dict(n_group=g, state_in=wide(state), **_wide(t))
+    y, out = torch.empty_like(dy), torch.empty_like(state)
+    aug.aug_scan_batch(off, **t, y_out=y, n_group=g, state_in=state, state_out=out)
+    with np.errstate(all="ignore"):
+        want, mag = R.scan(off, **args), R.scan(off, **args, magnitude=True)
+        gwant, gmag = (R.scan_backward(off, dy=wide(dy), magnitude=m, **args) for m in (False, True))
+    got = _gradients(aug, off, t, dy, g, state)
+    assert want[0][at, d] == np.inf and np.isfinite(gwant["du"][at - 1, d])
+    # Behind that row its channel holds infinities, which are lost where a decay is too small for 32 bits: not compared, nor what sums over
+    # them (db and dc of its group's states from that row on, the channel's parameters).
+    behind = np.zeros(len(dy), bool)
+    behind[at + 1:int(off[2])] = True
+    terms = S._terms(lengths, n)
+
+    def compare(what, k, ref, bound, extra):
+        ref, bound = ref.copy(), bound.copy()
+        g_ = wide(what).copy().reshape(ref.shape)
+        if k in ("y", "du", "ddelta", "dz"):
+            skip = np.zeros(ref.shape, bool)
+            skip[behind, d] = True
+            skip[at, d] = k != "y"
+        elif k in ("db", "dc"):
+            skip = np.zeros(ref.shape, bool)
+            skip[at:int(off[2]), (d // (dim // g)) * n:(d // (dim // g) + 1) * n] = True
+        else:
+            skip = np.zeros(ref.shape, bool)
+            if k == "state":
+                skip[1, d] = True
+            else:
+                skip[d] = True
+        for v in (ref, bound, g_):
+            v[skip] = 1.0
+        agrees(torch.from_numpy(g_).to(what.dtype), ref, bound, extra, k)
+
+    compare(y, "y", want[0], mag[0], terms)
+    compare(out, "state", want[1], mag[1], terms)
+    for k, v in got.items():
+        over = sum(lengths) if k in ("da", "dskip", "ddelta_bias") else dim // g if k in ("db", "dc") else 0
+        compare(v, k, gwant[k], gmag[k], 2 * terms + over)
+
+
+def _wide(t):
+    return {k: wide(v) for k, v in t.items()}
