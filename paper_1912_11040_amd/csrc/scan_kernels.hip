@@ -427,6 +427,28 @@ __global__ __launch_bounds__(256) void scan_back_sums_kernel(ScanArgs a, BackWs 
             back[k] = fmaf(q[k], sc[t][nq + k] * dp, back[k]);
         }
     }
+    // Decays that grow, by a rate above zero or a step below it, may take the product out of the range of 32 bits where no term is: the
+    // sum is then formed row by row from the last, as the definition does, and a term of zero stays zero.
+    bool lost = false;
+#pragma unroll
+    for (int k = 0; k < K; ++k) lost = lost || !(q[k] <= 3.4e38f);
+    if (!a.cfg.softplus) {
+        float least = 0.f, most = 0.f;
+        for (int t = 0; t < here; ++t) {
+            least = fminf(least, su[t][ch].x);
+            most = fmaxf(most, su[t][ch].x);
+        }
+        lost = lost || (least < 0.f && most > 0.f);      // what underflows may grow again
+    }
+    if (lost) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) back[k] = 0.f;
+#pragma unroll 1
+        for (int t = here - 1; t >= 0; --t) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) back[k] = pass_block(fmaf(sc[t][nq + k], sdp[t][ch], back[k]), 0.f, su[t][ch].x, rate[k]);
+        }
+    }
 #pragma unroll
     for (int k = 0; k < K; ++k)
         if (nq + k < n_state) ws.first[at + k] = f[k], ws.behind[at + k] = back[k];

@@ -94,3 +94,39 @@ def test_infinite_step(aug, lengths, last, n, name):
 
 def _wide(t):
     return {k: wide(v) for k, v in t.items()}
+
+
+# ---- states that grow beyond 32 bits inside a block of rows, where nothing is that grows, or next to nothing ----
+
+def _growing(dim, n, softplus, seed):
+    """A sequence of 150 rows in blocks of 32 or fewer: in rows 32 to 45 every state of the even channels grows by e^93 in all, more than the largest
+    32-bit number.  The input is zero up to row 95 and dy from row 32 on."""
+    off, _, t, _, dy = S._inputs([150, 40], dim, n, 1, torch.float32, seed, gate=False)
+    dy[32:150] = 0
+    t["u"][:96] = 0
+    t["a"][::2] = 0.5 if softplus else -0.5
+    t["delta"] = -t["delta"].abs() - 2 if softplus else t["delta"].abs() * 0.1
+    t["delta_bias"] = torch.zeros(dim, device="cuda")
+    t["delta"][32:46, ::2] = 12.0 if softplus else -12.0
+    t["delta"][36, ::2] = 30.0 if softplus else -30.0
+    return off, t, dy
+
+
+# the roundings of a decay's argument, its step's and its rate's among them, are relative to the argument: six of |step a| in every row
+GROWN = 6 * 93
+
+
+@pytest.mark.parametrize("softplus", [True, False])
+@pytest.mark.parametrize("n", [3, 16, 64, 100])
+@pytest.mark.parametrize("row,value", [(47, 0.0), (47, 1e-30)])
+def test_gradients_through_growing_decays(aug, row, value, n, softplus):
+    """The gradient that a block hands to the rows before it is zero times e^93, or 1e-30 times that."""
+    dim = 24
+    off, t, dy = _growing(dim, n, softplus, 50 + n)
+    dy[row] = value
+    args = dict(act="softplus" if softplus else "none", **_wide(t))
+    want, mag = (R.scan_backward(off, dy=wide(dy), magnitude=m, **args) for m in (False, True))
+    got = _gradients(aug, off, t, dy, 1, None, softplus)
+    for k, v in got.items():
+        over = 190 if k in ("da", "dskip", "ddelta_bias") else dim if k in ("db", "dc") else 0
+        agrees(v, want[k], mag[k], 2 * S._terms([150], n) + over + GROWN, k)
