@@ -198,9 +198,19 @@ template <int GROUPS> struct JoinShared {
 bool join_in_groups(int64_t width, int n_seq, int n_items, int n_cu) {
     return n_items / n_seq > 16 && width * n_seq < 64 * 8 * (int64_t)n_cu;       // fewer than eight wavefronts to a compute unit
 }
-__device__ inline float pass_block(float h, float value, float steps, float rate) {
-    // (a state of zero stays out of it, also where a rate above zero makes the factor infinite)
-    return h == 0.f ? value : fmaf(__builtin_amdgcn_exp2f(steps * rate), h, value);
+// A state of `h` through a block.  A rate above zero, or steps below it, may make the factor infinite: a state of zero stays out of it, and a
+// small one takes it by its root twice, which is infinite only where the state behind it is too unless the state is below 2^-128.
+// RARE: by a branch around the root (a batch's join, bound by memory; with the root always the gradients of 32 utterances take 690 us instead of 667);
+// else always (eight groups, whose chain is latency: a long recording 80 us, with the branch 85).
+template <bool RARE> __device__ inline float pass_block(float h, float value, float steps, float rate) {
+    const float factor = RARE ? __builtin_amdgcn_exp2f(steps * rate) : __builtin_amdgcn_exp2f(0.5f * steps * rate);
+    if (h == 0.f) return value;
+    if (!RARE) return fmaf(factor * h, factor, value);
+    if (__builtin_expect(factor > 3.4e38f, 0)) {
+        const float root = __builtin_amdgcn_exp2f(0.5f * steps * rate);
+        return fmaf(root * h, root, value);
+    }
+    return fmaf(factor, h, value);
 }
 template <int GROUPS>
 __device__ inline void join_blocks(JoinShared<GROUPS>& sh, float* values, const float* steps, int64_t width, int64_t i, int dim, int64_t d, float rate, float h,
@@ -221,7 +231,7 @@ __device__ inline void join_blocks(JoinShared<GROUPS>& sh, float* values, const 
             float value = 0.f, sum = 0.f;
 #pragma unroll
             for (int q = 0; q < kJoinAhead; ++q) {
-                value = pass_block(value, f[q], s[q], rate);
+                value = pass_block<false>(value, f[q], s[q], rate);
                 sum += s[q];
             }
             sh.value[group][lane] = value;
@@ -230,13 +240,13 @@ __device__ inline void join_blocks(JoinShared<GROUPS>& sh, float* values, const 
 #pragma unroll
             for (int g = 0; g < GROUPS; ++g) {
                 if (g == group) in = h;
-                h = pass_block(h, sh.value[g][lane], sh.steps[g][lane], rate);
+                h = pass_block<false>(h, sh.value[g][lane], sh.steps[g][lane], rate);
             }
         }
 #pragma unroll
         for (int q = 0; q < kJoinAhead; ++q) {
             if (i < width && j0 + q < n) values[(from + (int64_t)(j0 + q) * dir) * width + i] = in;
-            in = pass_block(in, f[q], s[q], rate);
+            in = pass_block<GROUPS == 1>(in, f[q], s[q], rate);
         }
         if constexpr (GROUPS > 1) {
             __syncthreads();
@@ -446,7 +456,7 @@ __global__ __launch_bounds__(256) void scan_back_sums_kernel(ScanArgs a, BackWs 
 #pragma unroll 1
         for (int t = here - 1; t >= 0; --t) {
 #pragma unroll
-            for (int k = 0; k < K; ++k) back[k] = pass_block(fmaf(sc[t][nq + k], sdp[t][ch], back[k]), 0.f, su[t][ch].x, rate[k]);
+            for (int k = 0; k < K; ++k) back[k] = pass_block<false>(fmaf(sc[t][nq + k], sdp[t][ch], back[k]), 0.f, su[t][ch].x, rate[k]);
         }
     }
 #pragma unroll
