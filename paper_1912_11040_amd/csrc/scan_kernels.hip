@@ -522,10 +522,12 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
     const bool gate = a.in.z.data;
     __syncthreads();
 
-    // A block's rows and what a lane reads of them.  The next block's are asked for behind the walk, when the states' registers are
+    // A block's rows and what a lane reads of them.  A short block's rows are the last ones of its RT: the ones in front of them have steps,
+    // inputs and gradients of zero and leave the first state as it is.  (Behind them they would meet the last row's state, which
+    // is in no gradient by the rates: a number or not.)  The next block's are asked for behind the walk, when the states' registers are
     // free, and where it lies a block earlier.
     struct Block {
-        int seq, here;
+        int seq, here, pad;
         int64_t begin;
     };
     struct Data {
@@ -534,14 +536,15 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
         float first[K], behind[K];
     };
     auto locate = [&](int it) -> Block {
-        if (it >= end_item) return {0, 0, 0};
+        if (it >= end_item) return {0, 0, 0, 0};
         const int2 item = a.rows.items[it];
         const int64_t begin = a.rows.begin[item.x] + ((int64_t)item.y << G::LG);
-        return {item.x, (int)min(a.rows.end[item.x] - begin, (int64_t)G::RT), begin};
+        const int here = (int)min(a.rows.end[item.x] - begin, (int64_t)G::RT);
+        return {item.x, here, G::RT - here, begin};
     };
     auto fetch = [&](const Block& blk, int it, Data& v) {
         if (blk.here <= 0) return;
-        const int64_t r = blk.begin + min(lt, blk.here - 1);
+        const int64_t r = blk.begin + max(lt - blk.pad, 0);
         v.u = load_part<T, G::EPT, FULL>(a.in.u, r, d0 + lc, width - lc);
         v.delta = load_part<T, G::EPT, FULL>(a.in.delta, r, d0 + lc, width - lc);
         v.dy = load_part<T, G::EPT, FULL>(a.dy, r, d0 + lc, width - lc);
@@ -549,8 +552,8 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
 #pragma unroll
         for (int j = 0; j < G::BC; ++j) {
             const int e = tid + 256 * j, t = e / G::NP, n = e % G::NP;
-            const bool there = t < blk.here && n < n_state;
-            const int64_t col = (int64_t)group * n_state + min(n, n_state - 1), at = blk.begin + min(t, blk.here - 1);
+            const bool there = t >= blk.pad && n < n_state;      // (what lies behind the tile is not kept either)
+            const int64_t col = (int64_t)group * n_state + min(n, n_state - 1), at = blk.begin + min(max(t - blk.pad, 0), blk.here - 1);
             const T b = row_in<T>(a.in.b, at)[col], c = row_in<T>(a.in.c, at)[col];
             v.b[j] = there ? b : (T)0;
             v.c[j] = there ? c : (T)0;
@@ -574,8 +577,8 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
             fetch(next_blk, it + 1, next_v);
             continue;
         }
-        const int valid = lt < here ? width - lc : 0;
-        const int64_t begin = blk.begin, r = begin + lt;
+        const int pad = blk.pad, first_stretch = pad / G::SUB, valid = lt >= pad ? width - lc : 0;
+        const int64_t begin = blk.begin, r = begin + lt - pad;
         const Pack<T, G::EPT> u = v.u, delta = v.delta, dy = v.dy, z = v.z;
 #pragma unroll
         for (int j = 0; j < G::BC; ++j) {
@@ -588,7 +591,7 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
         float carried[K];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            sst[0][tid][k] = v.first[k];
+            sst[first_stretch][tid][k] = v.first[k];
             carried[k] = v.behind[k];
         }
         float raw[G::EPT], step[G::EPT], dp[G::EPT];
@@ -604,7 +607,7 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
         }
 #pragma unroll
         for (int i = 0; i < G::EPT; ++i) {
-            // (rows behind the sequence are walked with steps and dp of zero)
+            // (rows in front of the block are walked with steps and dp of zero)
             step[i] = i < valid ? step[i] : 0.f;
             su[lt][lc + i] = make_float2(step[i], i < valid ? step[i] * (float)u.v[i] : 0.f);
             sdp[lt][lc + i] = i < valid ? dp[i] : 0.f;
@@ -616,7 +619,7 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
 #pragma unroll
             for (int k = 0; k < K; ++k) st[k] = v.first[k];
 #pragma unroll 1
-            for (int s = 1; s * G::SUB < here; ++s) {
+            for (int s = first_stretch + 1; s < NS; ++s) {
 #pragma unroll
                 for (int j = 0; j < G::SUB; ++j) {
                     const int t = (s - 1) * G::SUB + j;
@@ -628,9 +631,8 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
                 for (int k = 0; k < K; ++k) sst[s][tid][k] = SPARE && nq + k >= n_state ? 0.f : st[k];
             }
         }
-        // (rows behind the sequence's end inside a stretch have steps and dp of zero)
 #pragma unroll 1
-        for (int s = (here - 1) / G::SUB; s >= 0; --s) {
+        for (int s = NS - 1; s >= first_stretch; --s) {
             float h[G::SUB + 1][K], e[G::SUB][K];
 #pragma unroll
             for (int k = 0; k < K; ++k) h[0][k] = sst[s][tid][k];
@@ -755,7 +757,7 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
             par[i] = i < valid ? dp[i] * (float)u.v[i] : 0.f;
             par[G::EPT + i] = i < valid ? dstep[i] : 0.f;
         }
-        if (lt < here) {
+        if (lt >= pad) {
             if (a.grad.du.data) store_part<T, G::EPT, FULL>(a.grad.du, r, d0 + lc, du, valid);
             if (a.grad.ddelta.data) store_part<T, G::EPT, FULL>(a.grad.ddelta, r, d0 + lc, dd, valid);
             if (a.grad.dz.data) store_part<T, G::EPT, FULL>(a.grad.dz, r, d0 + lc, dz, valid);
@@ -765,8 +767,8 @@ __global__ __launch_bounds__(256, K <= 4 ? 2 : 1) void scan_back_kernel(ScanArgs
         for (int i = 0; i < kept<G::EPT>(); ++i) acc[i] += par[i];
         float* const bc = ws.bc + ((int64_t)tile * n_rows + begin) * 2 * n_state;
         for (int e = tid; e < here * 2 * G::NP; e += 256) {
-            const int t = e / (2 * G::NP), at = e % (2 * G::NP), n = at % G::NP;
-            if (n < n_state) bc[t * 2 * n_state + (at < G::NP ? n : n_state + n)] = (sbc[0][t][at] + sbc[1][t][at]) + (sbc[2][t][at] + sbc[3][t][at]);
+            const int row = e / (2 * G::NP), t = row + pad, at = e % (2 * G::NP), n = at % G::NP;
+            if (n < n_state) bc[row * 2 * n_state + (at < G::NP ? n : n_state + n)] = (sbc[0][t][at] + sbc[1][t][at]) + (sbc[2][t][at] + sbc[3][t][at]);
         }
         __syncthreads();
     }

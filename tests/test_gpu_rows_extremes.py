@@ -165,3 +165,24 @@ def test_states_and_gradients_through_blocks_that_grow(aug, n, rows):
     for k, v in _gradients(aug, off, t, dy, 1, None).items():
         over = rows + 40 if k in ("da", "dskip", "ddelta_bias") else dim if k in ("db", "dc") else 0
         agrees(v, want[k], mag[k], 2 * terms + over, k)
+
+
+# ---- what is no number in a sequence's last row ----
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("lengths,n", [([13], 16), ([40, 21, 3], 11), ([131, 65], 8), ([33, 7], 64), ([17, 30], 128)])
+def test_last_rows_state_has_no_part_in_the_rates_gradient(aug, lengths, n, value, name):
+    """An input that is no number in a sequence's last row reaches that row's state, which no row follows: the gradient by the rates has the states
+    before each row only, and stays what it is."""
+    dim, g = 68, 2
+    off, _, t, state, dy = S._inputs(lengths, dim, n, g, TYPES[name], 90 + n)
+    for i in range(len(lengths)):
+        t["u"][int(off[i + 1]) - 1, 5 + i] = value
+    args = dict(n_group=g, state_in=wide(state), **_wide(t))
+    with np.errstate(invalid="ignore"):
+        want, mag = (R.scan_backward(off, dy=wide(dy), magnitude=m, **args) for m in (False, True))
+    got = _gradients(aug, off, t, dy, g, state)
+    assert np.isfinite(want["da"]).all() and not np.isfinite(want["dskip"]).all()
+    agrees(got["da"], want["da"], mag["da"], 2 * S._terms(lengths, n) + sum(lengths), "da")
+    agrees(got["du"], want["du"], mag["du"], 2 * S._terms(lengths, n), "du")
