@@ -28,6 +28,30 @@ template <int TPR> __device__ inline float row_sum(float v, float* exchange) {
     return v;
 }
 
+// The largest of a row's lanes' values, in all of them.
+template <int TPR> __device__ inline unsigned row_max(unsigned v, float* exchange) {
+    v = lanes_max(v, TPR < 64 ? TPR : 64);
+    if constexpr (TPR > 64) {
+        __syncthreads();                                 // (the last ones have been read)
+        if (threadIdx.x % 64 == 0) exchange[threadIdx.x / 64] = __uint_as_float(v);
+        __syncthreads();
+        for (int i = 0; i < TPR / 64; ++i) v = max(v, __float_as_uint(exchange[i]));
+    }
+    return v;
+}
+
+template <int NV> __device__ inline float squares(const float (&s)[NV][kVec]) {
+    float ss = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        float part = 0.f;                                // (the squares of a stretch by themselves: shorter sums)
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) part = fmaf(s[j][i], s[j][i], part);
+        ss += part;
+    }
+    return ss;
+}
+
 template <class T, int TPR, int NV>
 __global__ __launch_bounds__(kThreads<TPR>) void norm_kernel(NormArgs a) {
     __shared__ float exchange[32];
@@ -53,16 +77,11 @@ __global__ __launch_bounds__(kThreads<TPR>) void norm_kernel(NormArgs a) {
             x[j] = load_pack<T, kVec>(row_in<T>(a.x, r) + c, dim - c);
             if (a.residual.data) res[j] = load_pack<T, kVec>(row_in<T>(a.residual, r) + c, dim - c);
         }
-        float ss = 0.f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int c = (j * TPR + lane) * kVec;
 #pragma unroll
             for (int i = 0; i < kVec; ++i) s[j][i] = (float)x[j].v[i] + (a.residual.data ? (float)res[j].v[i] : 0.f);
-            float part = 0.f;                            // (the squares of a stretch by themselves: shorter sums)
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) part = fmaf(s[j][i], s[j][i], part);
-            ss += part;
             if (a.sum.data) {
                 Pack<T, kVec> out;
 #pragma unroll
@@ -70,8 +89,30 @@ __global__ __launch_bounds__(kThreads<TPR>) void norm_kernel(NormArgs a) {
                 store_pack<T, kVec>(row_out<T>(a.sum, r) + c, out, dim - c);
             }
         }
-        const float rstd = 1.f / sqrtf(row_sum<TPR>(ss, exchange) / (float)dim + a.cfg.eps);
-        if (a.rstd && lane == 0) a.rstd[r] = rstd;
+        float total = row_sum<TPR>(squares(s), exchange), eps = a.cfg.eps;
+        int e = 0;
+        // Squares out of the range of 32 bits, where the row's values are not and eps does not outweigh what is lost: the row is divided by a
+        // power of two first, of its largest value or of eps' root.  (Nothing helps a row that holds a NaN or an infinity.)
+        if (!(total <= 3.4e38f) || (total < 0x1p-100f && eps < 0x1p-120f)) {
+            unsigned most = 0;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) most = max(most, __float_as_uint(s[j][i]) & 0x7fffffffu);
+            most = row_max<TPR>(most, exchange + 16);
+            if (most > 0 && most < 0x7f800000u) {
+                e = (int)(most >> 23) - 127;
+                if (eps > 0.f) e = max(e, ((int)(__float_as_uint(eps) >> 23) - 127) / 2);
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                    for (int i = 0; i < kVec; ++i) s[j][i] = ldexpf(s[j][i], -e);
+                total = row_sum<TPR>(squares(s), exchange);
+                eps = ldexpf(eps, -2 * e);
+            }
+        }
+        const float rstd = 1.f / sqrtf(total / (float)dim + eps);      // of the row divided by 2^e
+        if (a.rstd && lane == 0) a.rstd[r] = ldexpf(rstd, -e);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int c = (j * TPR + lane) * kVec;
@@ -99,13 +140,7 @@ __global__ __launch_bounds__(kThreads<TPR>) void norm_kernel(NormArgs a) {
         if (whole) {
 #pragma unroll
             for (int j = 1; j < NV; ++j) most[0] = most[0] > most[j] ? most[0] : most[j];
-            most[0] = lanes_max(most[0], TPR < 64 ? TPR : 64);
-            if constexpr (TPR > 64) {
-                __syncthreads();
-                if (threadIdx.x % 64 == 0) exchange[16 + threadIdx.x / 64] = __uint_as_float(most[0]);
-                __syncthreads();
-                for (int i = 0; i < TPR / 64; ++i) most[0] = max(most[0], __float_as_uint(exchange[16 + i]));
-            }
+            most[0] = row_max<TPR>(most[0], exchange + 16);
 #pragma unroll
             for (int j = 1; j < NV; ++j) most[j] = most[0];
         }

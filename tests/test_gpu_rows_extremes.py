@@ -186,3 +186,65 @@ def test_last_rows_state_has_no_part_in_the_rates_gradient(aug, lengths, n, valu
     assert np.isfinite(want["da"]).all() and not np.isfinite(want["dskip"]).all()
     agrees(got["da"], want["da"], mag["da"], 2 * S._terms(lengths, n) + sum(lengths), "da")
     agrees(got["du"], want["du"], mag["du"], 2 * S._terms(lengths, n), "du")
+
+
+# ---- rows whose squares are beyond 32 bits, and rows beyond whose squares nothing is ----
+
+LOUD = [1e30, 3e38, 2e19, 1.0, 3e16]
+QUIET = [1e-17, 1e-23, 1e-30, 1.0, 3e-38, 1e-41, 0.0]
+
+
+def _rows_of(dim, levels, dtype, seed):
+    """Rows of values between 2^-6 of a level and it, one of them the level itself, in the type and in 64 bits."""
+    rng = np.random.default_rng(seed)
+    v = rng.uniform(2.0 ** -6, 1.0, (len(levels), dim)) * rng.choice([-1.0, 1.0], (len(levels), dim))
+    v[:, dim // 2] = 1.0
+    x = torch.from_numpy(v * np.array(levels)[:, None]).to(dtype)
+    assert torch.isfinite(x).all()
+    return x.cuda()
+
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("dim,q_block", [(1, 0), (40, 16), (100, 0), (500, 64), (1001, 128), (3000, 0), (4100, 512), (9000, 0), (16384, 256)])
+@pytest.mark.parametrize("levels,eps", [(LOUD, 1e-6), (LOUD, 0.0), (LOUD, 1e38), (QUIET, 0.0), (QUIET, 1e-38), (QUIET, 1e-30), (QUIET, 1e-6)])
+def test_norm_beyond_the_range_of_squares(aug, levels, eps, dim, q_block, name):
+    dtype = TYPES[name]
+    x = _rows_of(dim, levels, dtype, dim)
+    w = torch.linspace(0.5, 1.5, dim, device="cuda")
+    rows, width = len(levels), q_block or dim
+    y, q = torch.empty_like(x), torch.empty(rows, dim, dtype=torch.float8_e4m3fn, device="cuda")
+    scale, rstd = torch.empty(rows, -(-dim // width), device="cuda"), torch.empty(rows, device="cuda")
+    aug.aug_rms_norm_batch(x, w, eps=eps, y_out=y, q_out=q, scale_out=scale, rstd_out=rstd, q_block=q_block)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        # (eps as the call gets it)
+        _, want, r = R.rms_norm(wide(x), None, wide(w), float(np.float32(eps)))
+    # a reciprocal root beyond 32 bits is infinite, one below 2^-126 has the step of those
+    r = np.where(r > np.finfo(np.float32).max, np.inf, r)
+    terms = dim / 2 + 16
+    agrees(rstd, r, np.abs(r), terms, "rstd")
+    agrees(y, want, np.abs(want), terms, "y")
+    if levels[-1] == 0.0 and eps == 0.0:
+        want = want[:-1]                                  # (zero by zero)
+        assert np.isnan(wide(scale)[-1]).all()
+    n = len(want)
+    scales = R.block_scales(want, q_block)
+    agrees(scale[:n], scales, scales, terms + 2, "scale")
+    by = np.repeat(wide(scale)[:n], width, axis=1)[:, :dim]
+    v = np.divide(want, by, out=np.zeros_like(want), where=by >= 2.0 ** -126)
+    seen = by >= 2.0 ** -126                              # (scales of at least the smallest normal number)
+    got = wide(q.float())[:n]
+    assert np.all(np.abs(got - v)[seen] <= (np.maximum(2.0 ** -4 * np.abs(v), 2.0 ** -10) + (terms + 4) * 2.0 ** -24 * np.abs(v))[seen])
+
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+def test_norm_of_a_row_with_one_loud_value(aug, name):
+    """One value of 1e30 among ordinary ones: the row's scale is that value's, and no other row's."""
+    x = torch.randn(4, 96, device="cuda").to(TYPES[name])
+    x[3, 5] = 1e30
+    y, q, scale, rstd = torch.empty_like(x), torch.empty(4, 96, dtype=torch.float8_e4m3fn, device="cuda"), torch.empty(4, 3, device="cuda"), torch.empty(4, device="cuda")
+    aug.aug_rms_norm_batch(x, None, y_out=y, q_out=q, scale_out=scale, rstd_out=rstd, q_block=32)
+    _, want, r = R.rms_norm(wide(x))
+    agrees(rstd, r, r, 64, "rstd")
+    agrees(y, want, np.abs(want), 64, "y")
+    agrees(scale, R.block_scales(want, 32), R.block_scales(want, 32), 66, "scale")
+    assert wide(q.float())[3, 5] == 448.0 and wide(y)[3, 5] > 9.7
