@@ -194,21 +194,22 @@ __global__ __launch_bounds__(kThreads<TPR>) void norm_backward_kernel(NormBackAr
             float part = 0.f;
 #pragma unroll
             for (int i = 0; i < kVec; ++i) {
-                const float xi = (float)x[j].v[i], g = (float)dy[j].v[i];
+                const float xi = (float)x[j].v[i] * rstd, g = (float)dy[j].v[i];
                 part = fmaf(xi, g * w[j][i], part);
-                dw[j][i] = fmaf(g, xi * rstd, dw[j][i]);
+                dw[j][i] = fmaf(g, xi, dw[j][i]);
             }
             dot += part;
         }
         if (!a.dx.data) continue;
-        const float slope = row_sum<TPR>(dot, exchange) / (float)dim * rstd * rstd * rstd;
+        // dx = rstd (w dy - x rstd mean(x rstd w dy)): the powers of rstd by themselves leave the range of 32 bits at rows of 1e13
+        const float slope = row_sum<TPR>(dot, exchange) / (float)dim;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int c = (j * TPR + lane) * kVec;
             Pack<T, kVec> out;
 #pragma unroll
             for (int i = 0; i < kVec; ++i) {
-                float g = fmaf((float)dy[j].v[i] * w[j][i], rstd, -(float)x[j].v[i] * slope);
+                float g = rstd * fmaf(-(float)x[j].v[i] * rstd, slope, (float)dy[j].v[i] * w[j][i]);
                 if (a.dsum.data) g += (float)ds[j].v[i];
                 out.v[i] = (T)g;
             }

@@ -248,3 +248,20 @@ def test_norm_of_a_row_with_one_loud_value(aug, name):
     agrees(y, want, np.abs(want), 64, "y")
     agrees(scale, R.block_scales(want, 32), R.block_scales(want, 32), 66, "scale")
     assert wide(q.float())[3, 5] == 448.0 and wide(y)[3, 5] > 9.7
+
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [1, 40, 500, 1001, 3000, 9000])
+def test_norm_gradients_of_loud_and_quiet_rows(aug, dim, name):
+    """Rows of 1e30 to 1e-30, whose reciprocal roots' third powers are beyond 32 bits: both terms of the gradient are there."""
+    levels = [1e30, 3e18, 1e13, 1e6, 1.0, 1e-6, 1e-13, 1e-20, 1e-30]
+    x = _rows_of(dim, levels, TYPES[name], dim)
+    dy = _rows_of(dim, [1.0] * len(levels), TYPES[name], dim + 1)
+    w = torch.linspace(0.5, 1.5, dim, device="cuda")
+    rstd = torch.from_numpy(R.rms_norm(wide(x), eps=0.0)[2]).float().cuda()
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    aug.aug_rms_norm_backward_batch(x, rstd, dy, w, dx_out=dx, dweight_out=dw)
+    args = (wide(x), wide(rstd), wide(dy), wide(w))
+    want, mag = R.rms_norm_backward(*args), R.rms_norm_backward(*args, magnitude=True)
+    agrees(dx, want[0], mag[0], dim + 16, "dx")
+    agrees(dw, want[1], mag[1], len(levels) + 16, "dweight")
