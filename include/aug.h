@@ -375,8 +375,8 @@ typedef struct aug_norm_cfg {
  *   y_out      y, or null.  May be x or residual (the same matrix, with the same ld).
  *   q_out      y in 8 bits (OCP e4m3, one byte per element, ld in bytes), or null; then
  *   scale_out  DEVICE float [n_rows][ceil(dim / q_block)], required with q_out: scale = max |y| / 448 over the
- *              block's columns, q = y / scale rounded to nearest even, 0 where scale is 0.  y goes into both
- *              unrounded.  A block that holds a NaN or an infinity has a scale that is none either.
+ *              block's columns (rounded up where it is below the normal numbers), q = y / scale rounded to nearest even,
+ *              0 where scale is 0.  y goes into both unrounded.  A block that holds a NaN or an infinity has a scale that is none either.
  *   rstd_out   DEVICE float [n_rows] or null: what the gradients need.
  */
 int aug_rms_norm_batch(aug_ctx* ctx, int64_t n_rows, const aug_norm_cfg* cfg, const aug_rows* x, const aug_rows* residual,

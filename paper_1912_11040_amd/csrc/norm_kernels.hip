@@ -148,7 +148,9 @@ __global__ __launch_bounds__(kThreads<TPR>) void norm_kernel(NormArgs a) {
         for (int j = 0; j < NV; ++j) {
             const int c = (j * TPR + lane) * kVec;
             if (!whole) most[j] = lanes_max(most[j], width / kVec);
-            const float scale = __uint_as_float(most[j]) / 448.f;
+            float scale = __uint_as_float(most[j]) / 448.f;
+            // (below the normal numbers a quotient rounded down may leave y / scale beyond e4m3's largest number: rounded up there)
+            if (scale < 0x1p-126f && scale * 448.f < __uint_as_float(most[j])) scale = __uint_as_float(__float_as_uint(scale) + 1);
             if (c < dim && (whole ? c == 0 : c % width == 0)) a.scale[r * n_blocks + (whole ? 0 : c / width)] = scale;
             const float by = scale == 0.f ? 1.f : scale;
             Pack<unsigned, 2> out;

@@ -265,3 +265,25 @@ def test_norm_gradients_of_loud_and_quiet_rows(aug, dim, name):
     want, mag = R.rms_norm_backward(*args), R.rms_norm_backward(*args, magnitude=True)
     agrees(dx, want[0], mag[0], dim + 16, "dx")
     agrees(dw, want[1], mag[1], len(levels) + 16, "dweight")
+
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("dim,q_block", [(40, 16), (100, 0), (1001, 128), (4100, 0)])
+@pytest.mark.parametrize("level", [1e-39, 1e-40, 1e-41, 3e-42, 3e-43, 1e-44])
+def test_scales_below_the_normal_numbers(aug, level, dim, q_block, name):
+    """Outputs so small that their scale is one of few bits: it is none less than the block's largest value over 448, so that codes are numbers."""
+    x = _rows_of(dim, [1.0, 1.0], TYPES[name], dim)
+    w = torch.full((dim,), level, device="cuda")
+    q, width = torch.empty(2, dim, dtype=torch.float8_e4m3fn, device="cuda"), q_block or dim
+    scale = torch.empty(2, -(-dim // width), device="cuda")
+    aug.aug_rms_norm_batch(x, w, q_out=q, scale_out=scale, q_block=q_block)
+    _, want, _ = R.rms_norm(wide(x), None, wide(w))
+    exact, got = R.block_scales(want, q_block), wide(scale)
+    # y is off by half a step of 2^-149 and 64 + dim / 2 roundings, the quotient is rounded up
+    tol = 2.0 ** -150 / 448 + (dim / 2 + 64) * 2.0 ** -24 * exact
+    assert np.all(got >= exact - tol) and np.all(got <= exact + tol + 2.0 ** -149)
+    by = np.repeat(got, width, axis=1)[:, :dim]
+    v, codes = np.divide(want, by, out=np.zeros_like(want), where=by > 0), wide(q.float())
+    assert np.isfinite(codes).all()
+    off = np.divide(2.0 ** -150, by, out=np.zeros_like(want), where=by > 0) + (dim / 2 + 64) * 2.0 ** -24 * np.abs(v)
+    assert np.all(np.abs(codes - v) <= np.maximum(2.0 ** -4 * (np.abs(v) + off), 2.0 ** -10) + off)
