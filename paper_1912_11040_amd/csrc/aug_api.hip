@@ -583,6 +583,7 @@ int aug_destroy(aug_ctx* ctx) {
     for (DeviceBuffer& b : ctx->d_frame_items) b.release();
     for (DeviceBuffer& b : all.rows.d_first) b.release();
     for (DeviceBuffer& b : all.rows.d_items) b.release();
+    for (auto& o : all.rows.orders) o.d_items.release();
     for (DeviceBuffer& b : ctx->twiddle) b.release();
     for (DeviceBuffer& b : ctx->conv_tab) b.release();
     for (auto& m : ctx->marks) (void)hipEventDestroy(m.first);

@@ -110,8 +110,8 @@ struct Sequences {
     const int64_t *offsets, *lengths;
     int64_t n_rows = 0;                  // rows up to the last sequence's end
     int64_t total = 0;                   // rows of the sequences
-    int abreast = 1;                     // whole sequences that the chip takes side by side
     RowBlocks blocks;
+    size_t order = 0;                    // the table of whole sequences
     bool new_rows = false, new_table = false;
 
     Sequences(aug_ctx* c, int n, const int64_t* o, const int64_t* l) : ctx(c), n_seq(n), offsets(o), lengths(l) {
@@ -122,8 +122,9 @@ struct Sequences {
     }
     int64_t end(int i) const { return lengths ? offsets[i] + lengths[i] : offsets[i + 1]; }
 
-    // Cut into blocks of 1 << lg rows, each of which `tiles` work groups share.  Memory is found here, nothing is launched.
-    int plan(int lg, int tiles) {
+    // Cut into blocks of 1 << lg rows, each of which `tiles` work groups share; left whole, `abreast` of them are taken side by side.
+    // Memory is found here, nothing is launched.
+    int plan(int lg, int tiles, int abreast = 1) {
         aug::RowTables& t = aug::whole(ctx).rows;
         const size_t n = (size_t)n_seq + 1;
         bool same = t.begin.size() == n && !memcmp(t.begin.data(), offsets, n * sizeof(int64_t));
@@ -135,7 +136,17 @@ struct Sequences {
         blocks.lg = lg;
         blocks.n_items = (int)items;
         new_rows = n_seq > 0 && !same;
-        new_table = n_seq > 0 && (new_rows || t.n_items[lg] == 0);
+        const bool whole = lg == aug::kWholeLg;
+        if (whole) {
+            if (abreast >= n_seq) abreast = 0;
+            for (order = 0; order < t.orders.size() && t.orders[order].abreast != abreast;) ++order;
+            if (order == t.orders.size()) {
+                t.orders.emplace_back();
+                t.orders[order].abreast = abreast;
+            }
+        }
+        const bool there = whole ? t.orders[order].there : t.n_items[lg] > 0;
+        new_table = n_seq > 0 && (new_rows || !there);
         if (new_table) {
             hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
             if (hipStreamIsCapturing(ctx->stream, &st) != hipSuccess) (void)hipGetLastError();
@@ -143,19 +154,18 @@ struct Sequences {
                 return fail(ctx, AUG_ERR_UNSUPPORTED, "the tables for these rows are not there: they cannot be built while the stream is "
                             "being captured (run the same call once before capturing it)");
             if (new_rows) {              // (the record is true again once the tables are launched)
-                t.begin.clear();
-                std::memset(t.n_items, 0, sizeof t.n_items);
+                t.forget();
                 AUG_TRY(grow(ctx, t.d_begin, n * sizeof(int64_t), "row offsets buffer"));
                 AUG_TRY(grow(ctx, t.d_end, n * sizeof(int64_t), "row ends buffer"));
             }
-            AUG_TRY(grow(ctx, t.d_first[lg], n * sizeof(int), "row block prefix table"));
-            AUG_TRY(grow(ctx, t.d_items[lg], (size_t)items * sizeof(int2), "row block table"));
+            if (!whole) AUG_TRY(grow(ctx, t.d_first[lg], n * sizeof(int), "row block prefix table"));
+            AUG_TRY(grow(ctx, whole ? t.orders[order].d_items : t.d_items[lg], (size_t)items * sizeof(int2), "row block table"));
             AUG_TRY(aug::ring_reserve(ctx, aug::ring_bytes(n)));
         }
         blocks.begin = t.d_begin.as<int64_t>();
         blocks.end = t.d_end.as<int64_t>();
-        blocks.first = t.d_first[lg].as<int>();
-        blocks.items = t.d_items[lg].as<int2>();
+        blocks.first = whole ? nullptr : t.d_first[lg].as<int>();
+        blocks.items = (whole ? t.orders[order].d_items : t.d_items[lg]).as<int2>();
         return AUG_OK;
     }
 
@@ -178,8 +188,8 @@ struct Sequences {
         ta.whole = whole;
         ta.d_begin = t.d_begin.as<int64_t>();
         ta.d_end = t.d_end.as<int64_t>();
-        ta.d_first = t.d_first[blocks.lg].as<int>();
-        ta.items = t.d_items[blocks.lg].as<int2>();
+        ta.d_first = whole ? nullptr : t.d_first[blocks.lg].as<int>();
+        ta.items = (whole ? t.orders[order].d_items : t.d_items[blocks.lg]).as<int2>();
         if (new_rows) {
             memcpy(h, offsets, i64);
             for (int i = 0; i < n_seq; ++i) t.end[i] = end(i);
@@ -191,8 +201,7 @@ struct Sequences {
         int* const first = reinterpret_cast<int*>(h + 2 * i64);
         int at = 0;
         if (whole) {
-            order(first);
-            at = n_seq;
+            place(first, t.orders[order].abreast);
         } else {
             for (int i = 0; i < n_seq; ++i) {
                 first[i] = at;
@@ -203,14 +212,16 @@ struct Sequences {
         ta.first = reinterpret_cast<const int*>(d + 2 * i64);
         AUG_HIP(aug::launch_row_tables(ctx->stream, ta), "row tables kernel");
         if (new_rows) t.begin.assign(offsets, offsets + n);
-        t.n_items[blocks.lg] = at;
+        if (whole) t.orders[order].there = true;
+        else t.n_items[blocks.lg] = at;
         return aug::packing_launched(ctx);
     }
 
   private:
-    // Places of whole sequences: the long ones first, `abreast` of them side by side in turn forth and back, so that a compute unit's sequences
-    // add up alike.  (64 sequences of 98 to 1598 rows in the order they came in: the unluckiest had half as many rows again as the mean.)
-    void order(int* place) const {
+    // Places of whole sequences: the long ones first, `abreast` of them (0: all) side by side in turn forth and back, so that a compute
+    // unit's sequences add up alike.  (64 sequences of 98 to 1598 rows in the order they came in: the unluckiest had half as many rows again as the mean.)
+    void place(int* at, int abreast) const {
+        if (!abreast) abreast = n_seq;
         std::vector<int> by_length(n_seq);
         for (int i = 0; i < n_seq; ++i) by_length[i] = i;
         std::sort(by_length.begin(), by_length.end(), [&](int i, int j) {
@@ -219,7 +230,7 @@ struct Sequences {
         });
         for (int p = 0; p < n_seq; ++p) {
             const int turn = p / abreast, from = turn * abreast, to = std::min(from + abreast, n_seq);
-            place[by_length[p]] = turn % 2 ? to - 1 - (p - from) : p;
+            at[by_length[p]] = turn % 2 ? to - 1 - (p - from) : p;
         }
     }
     int64_t blocks_of(int i, int lg) const {
@@ -499,8 +510,8 @@ int aug_scan_batch(aug_ctx* ctx, int n_seq, const int64_t* row_offsets, const in
         sp.add("y_out", a.y.data, a.y.ld * e, cfg->dim * e, seq.n_rows, 1, 0);
         AUG_TRY(sp.check(ctx));
         if (n_seq == 0 || (seq.total == 0 && !state_out)) return AUG_OK;
-        AUG_TRY(seq.plan(aug::scan_lg_block(*cfg, n_seq, row_offsets, row_lengths, ctx->n_cu, false), aug::scan_tiles(*cfg, false)));
-        seq.abreast = aug::scan_abreast(*cfg, ctx->n_cu);
+        AUG_TRY(seq.plan(aug::scan_lg_block(*cfg, n_seq, row_offsets, row_lengths, ctx->n_cu, false), aug::scan_tiles(*cfg, false),
+                         aug::scan_abreast(*cfg, ctx->n_cu)));
         if (seq.blocks.lg != aug::kWholeLg) {        // whole sequences need none
             AUG_TRY(grow(ctx, aug::whole(ctx).seq_ws, aug::scan_workspace(*cfg, seq.blocks.n_items, seq.n_rows, ctx->n_cu, false), "scan workspace"));
             a.ws = aug::whole(ctx).seq_ws.ptr;

@@ -10,11 +10,23 @@ namespace aug {
 struct RowTables {
     std::vector<int64_t> begin;          // n_seq + 1, as given
     std::vector<int64_t> end;            // n_seq + 1: end of each sequence (the last entry counts for nothing)
-    static constexpr int kTables = 31;   // blocks of 1 .. 2^30 rows
+    static constexpr int kTables = 30;   // blocks of 1 .. 2^29 rows
     int n_items[kTables] = {};           // blocks; 0: the table is not there
     DeviceBuffer d_begin, d_end;         // int64 [n_seq+1]
     DeviceBuffer d_first[kTables];       // int [n_seq+1]: blocks of the sequences before i
     DeviceBuffer d_items[kTables];       // int2 [n_items]: (sequence, block of it)
+    // Whole sequences: a table per number of them that calls take side by side (0: all of them), which its order depends on.
+    struct Order {
+        int abreast = 0;
+        bool there = false;
+        DeviceBuffer d_items;            // int2 [n_seq]
+    };
+    std::vector<Order> orders;
+    void forget() {
+        begin.clear();
+        for (int& n : n_items) n = 0;
+        for (Order& o : orders) o.there = false;
+    }
 };
 
 // What aug_create makes: the waveform path's context with the row operators' share of it.
@@ -33,7 +45,7 @@ struct RowBlocks {
     const int2* items = nullptr;         // device [n_items]: (sequence, block of it)
 };
 
-constexpr int kWholeLg = 30;             // blocks of whole sequences
+constexpr int kWholeLg = RowTables::kTables;      // blocks of whole sequences, which are shorter than 2^30 rows
 
 // The device's tables of a batch of sequences from what the host left in pinned memory: begin and end (null: they are there already)
 // and the exclusive prefix sum of the blocks, n_seq + 1 entries each.  With `whole`, a block per sequence, `first` gives instead the
