@@ -287,3 +287,43 @@ def test_scales_below_the_normal_numbers(aug, level, dim, q_block, name):
     assert np.isfinite(codes).all()
     off = np.divide(2.0 ** -150, by, out=np.zeros_like(want), where=by > 0) + (dim / 2 + 64) * 2.0 ** -24 * np.abs(v)
     assert np.all(np.abs(codes - v) <= np.maximum(2.0 ** -4 * (np.abs(v) + off), 2.0 ** -10) + off)
+
+
+# ---- steps of both signs, all values well within 32 bits ----
+
+def _signed(lengths, dim, n, g, dtype, seed):
+    off, _, t, state, dy = S._inputs(lengths, dim, n, g, dtype, seed, plain=True)
+    t["a"] = t["a"] * (1.5 / t["a"].abs().max())          # so that a row's decay is e^3 at most, and a long sequence's product e^20
+    t["delta"] = t["delta"] * 0.5
+    return off, t, state, dy
+
+
+@pytest.mark.parametrize("name", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("n_seq,dim,n,g", [(4, 10, 128, 5), (9, 66, 100, 3), (33, 64, 64, 1), (5, 40, 16, 1), (7, 20, 3, 2)])
+def test_streams_with_steps_of_both_signs(aug, n_seq, dim, n, g, name):
+    off, t, state, _ = _signed([1] * n_seq, dim, n, g, TYPES[name], 7 * n_seq + n)
+    y, out = torch.empty_like(t["u"]), torch.empty_like(state)
+    aug.aug_scan_step(**t, state_in=state, state_out=out, y_out=y, n_group=g, softplus=False)
+    args = dict(n_group=g, state_in=wide(state), act="none", **_wide(t))
+    want, mag = R.scan(off, **args), R.scan(off, **args, magnitude=True)
+    assert mag[0].max() < 6e4 and mag[1].max() < 6e4      # every element is compared, in every type
+    agrees(y, want[0], mag[0], S._terms([1], n) + 18, "y")             # (six of the decay's argument, which is 3 at most)
+    agrees(out, want[1], mag[1], S._terms([1], n) + 18, "state")
+
+
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+@pytest.mark.parametrize("lengths,dim,n,g", [([70, 5, 33], 72, 16, 1), ([300], 66, 11, 3), ([100, 40], 24, 128, 2), ([64, 64], 64, 64, 1)])
+def test_gradients_with_steps_of_both_signs(aug, lengths, dim, n, g, name):
+    off, t, state, dy = _signed(lengths, dim, n, g, TYPES[name], dim + n)
+    args = dict(n_group=g, state_in=wide(state), act="none", **_wide(t))
+    want, mag = R.scan(off, **args), R.scan(off, **args, magnitude=True)
+    argument = 6 * max(np.abs(args["delta"][a:b, :, None] * args["a"][None]).sum(0).max() for a, b in R.spans(off) if b > a)
+    terms = S._terms(lengths, n) + argument
+    y, out = torch.empty_like(dy), torch.empty_like(state)
+    aug.aug_scan_batch(off, **t, y_out=y, n_group=g, softplus=False, state_in=state, state_out=out)
+    agrees(y, want[0], mag[0], terms, "y")
+    agrees(out, want[1], mag[1], terms, "state")
+    want, mag = (R.scan_backward(off, dy=wide(dy), magnitude=m, **args) for m in (False, True))
+    for k, v in _gradients(aug, off, t, dy, g, state, softplus=False).items():
+        over = sum(lengths) if k in ("da", "dskip", "ddelta_bias") else dim // g if k in ("db", "dc") else 0
+        agrees(v, want[k], mag[k], 2 * terms + over, k)
