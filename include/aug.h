@@ -340,7 +340,8 @@ int aug_pipeline_batch(aug_ctx* ctx, int n_utt, const int64_t* offsets, const fl
  *     row_offsets[i] of every matrix.  row_lengths HOST int64 [n_seq] gives their numbers, at most row_offsets[i+1] -
  *     row_offsets[i]; null: exactly that many.  frame_offsets of the front end are row_offsets; for its padded layout
  *     give the frame counts as row_lengths.  Rows that belong to no sequence are neither read nor written.  Lengths of
- *     0 are allowed; n_seq <= AUG_MAX_UTT and a sequence < 2^30 rows (AUG_ERR_UNSUPPORTED otherwise).
+ *     0 are allowed; n_seq <= AUG_MAX_UTT and a sequence < 2^30 rows (AUG_ERR_UNSUPPORTED otherwise).  So is a call of
+ *     2^24 work groups or more, of which each takes 16 rows (or a sequence) of 16 channels (or a group's) at the least.
  *   - Outputs must not overlap inputs or one another (AUG_ERR_INVALID_ARG) except where an argument says so.
  *     Column slices of one matrix that share no column do not overlap.
  *   - The same call gives the same bits: no sum is formed by floating-point atomics.
@@ -378,6 +379,8 @@ typedef struct aug_norm_cfg {
  *              block's columns (rounded up where it is below the normal numbers), q = y / scale rounded to nearest even,
  *              0 where scale is 0.  y goes into both unrounded.  A block that holds a NaN or an infinity has a scale that is none either.
  *   rstd_out   DEVICE float [n_rows] or null: what the gradients need.
+ * A row of finite s is normed whatever its magnitude, also where its squares are beyond 32 bits; an rstd that is
+ * beyond them is infinite.  A row that holds an infinity or a NaN has an rstd of 0 or NaN.
  */
 int aug_rms_norm_batch(aug_ctx* ctx, int64_t n_rows, const aug_norm_cfg* cfg, const aug_rows* x, const aug_rows* residual,
                        const float* weight, const aug_rows* sum_out, const aug_rows* y_out, const aug_rows* q_out,
@@ -462,6 +465,8 @@ typedef struct aug_scan_in {
  *   state_out  h behind each sequence's last row (state_in's where it has none).  May be state_in; null if not wanted.
  *   y_out      dim columns.
  * Long sequences are cut into stretches that run side by side: a call with few sequences needs workspace for a state per stretch.
+ * exp(step a) is a 32-bit number: where step a is beyond 88, by a positive rate or a negative step, it is infinite and
+ * makes NaN of a state of zero.
  */
 int aug_scan_batch(aug_ctx* ctx, int n_seq, const int64_t* row_offsets, const int64_t* row_lengths, const aug_scan_cfg* cfg,
                    const aug_scan_in* in, const float* state_in, float* state_out, const aug_rows* y_out);
@@ -475,6 +480,7 @@ typedef struct aug_scan_grad {
 /*
  * Gradients of aug_scan_batch from dy.  in and state_in are what the forward call had; state_in counts as a constant and
  * no gradient comes in by state_out.  No forward result is needed: states are computed anew.  dz must be null without a gate.
+ * The workspace holds two states per 32 rows (16 with more than 64 states) and, for every row and tile of 16 to 64 channels, 2 n_state floats.
  */
 int aug_scan_backward_batch(aug_ctx* ctx, int n_seq, const int64_t* row_offsets, const int64_t* row_lengths,
                             const aug_scan_cfg* cfg, const aug_scan_in* in, const float* state_in, const aug_rows* dy,
@@ -492,6 +498,7 @@ int aug_scan_step(aug_ctx* ctx, int n_seq, const aug_scan_cfg* cfg, const aug_sc
  * milliseconds of every stage recorded since the last read into
  * ms_out[AUG_N_STAGES] (HOST float) and the number of times each stage ran into
  * launches_out[AUG_N_STAGES] (HOST int32, may be NULL), then forgets them.
+ * AUG_N_STAGES grows with the stages: callers are built with the header of the library that they load.
  */
 enum {
     AUG_STAGE_RIR = 0,        /* image-sum kernel */

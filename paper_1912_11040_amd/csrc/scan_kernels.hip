@@ -28,8 +28,8 @@ __device__ inline float rate2(float a) {
 //
 //   h = exp(step a) h + step u b,   y = (sum c h + skip u) z sigmoid(z)
 // A state's row is a product, an exponential (four issue slots), a product and two multiply-adds: at sixteen states 128 slots a
-// (row, channel) against 8 bytes of 16-bit rows, so vector issue bounds it (64 utterances of 98 to 1598 rows, 1024 channels, bf16: 249 us, 86 % of
-// the slots busy; their bytes would take 97 us at the rate of a copy).
+// (row, channel) against 8 bytes of 16-bit rows, so vector issue bounds it (64 utterances of 98 to 1598 rows, 1024 channels, bf16: 240 us, with vector
+// instructions under way all the time that its compute units are busy; their bytes would take 97 us at the rate of a copy).
 // A group of four wavefronts takes 256 / LN channels through a block of rows; LN neighbouring lanes share a channel, K states each
 // in registers, and add up their part of the output.  (A lane per channel would need no sums and a quarter of the groups; the chip is
 // hard to fill as it is.)  Rows come in tiles of TT: all lanes turn EPT elements each of u and delta into steps and step u in LDS, once
@@ -313,9 +313,11 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, int n_seq, i
 // the block's share of e_first g_first, which is what it hands to the rows before it.  scan_back_join_kernel then makes of F the state
 // before each block and of R what comes in from behind.  With both the blocks are independent of one another: the main pass
 // walks a block forward for its states and back for its gradients, in stretches of SUB rows whose states and decays stay in registers.
-// Both are bound by vector issue: 32 utterances of 98 to 1598 rows, 1024 channels, 16 states, bf16 take 165 us (80 % of the slots) and 473 (76 %),
-// the join between them 49 (HBM), 670 in all.  In blocks of 32 rows the sums are 8 of the 30 bytes moved a (row, channel); stretches of 16
-// rows need more registers than two wavefronts per SIMD leave (1250 us with one).
+// Both are bound by vector issue: 32 utterances of 98 to 1598 rows, 1024 channels, 16 states, bf16 take 155 us (vector instructions under way 93 % of
+// the time) and 440 (87 %), the join between them 51 (HBM), the sums over tiles and runs 19, 665 in all.  In blocks of 32 rows the sums are 8 of the 30 bytes moved a (row, channel); stretches of 16
+// rows need more registers than two wavefronts per SIMD leave (1250 us with one).  So do, by 14 to 22 registers, which the compiler keeps in
+// scratch, stretches of eight rows at four states a lane where a partial tile's accesses or 32-bit elements come on top; 16-bit ones of
+// whole tiles do without.
 template <int LN, int K> struct BackTile {
     static constexpr int CW = 256 / LN, NP = LN * K, LG = NP <= 64 ? 5 : 4, RT = 1 << LG, EPT = RT * CW / 256, SUB = K <= 2 ? 16 : 8;
     static constexpr int BC = (RT * NP + 255) / 256;
@@ -848,8 +850,11 @@ int scan_lg_block(const aug_scan_cfg& cfg, int n_seq, const int64_t* begin, cons
     if (backward) return cfg.n_state <= 64 ? 5 : 4;      // BackTile
     // Sixteen states: a compute unit with several groups takes some 75 ns for a row of one, a group by itself 136 ns (the latency of its chain), so
     // that a whole sequence takes no less than its length of those.  In blocks the walk is done nearly twice (end states, then outputs),
-    // some 143 ns a row, with two launches more.  (Four sequences of 4000 rows, 2048 channels: whole 543 us, in blocks 241; 32 of 800, 1024
-    // channels: 143 and 201.)
+    // some 143 ns a row, with two launches more.  (Four sequences of 4000 rows, 2048 channels: whole 501 us, in blocks 235; 32 of 800, 1024
+    // channels: 132 and 193; 16 of 800: 102 and 110.)  The other numbers of states follow the same rule, by their own tiles: 4 states 960 and 135,
+    // 190 and 109, 190 and 76; 32 states 741 and 379, 201 and 311, 152 and 177; 128 states 1105 and 1340, 666 and 1059, 365 and 605.  It is wrong
+    // by a fifth where 64 states leave it few long sequences (the first of these: taken whole 826, in blocks 666) and by a tenth for 64 of
+    // 800 rows with 4 states (whole 223, in blocks 198).
     int64_t rows = 0, longest = 0;
     for (int i = 0; i < n_seq; ++i) {
         const int64_t len = lengths ? lengths[i] : begin[i + 1] - begin[i];
