@@ -196,9 +196,10 @@ __global__ __launch_bounds__(kThreads<TPR>) void norm_backward_kernel(NormBackAr
             float part = 0.f;
 #pragma unroll
             for (int i = 0; i < kVec; ++i) {
-                const float xi = (float)x[j].v[i] * rstd, g = (float)dy[j].v[i];
-                part = fmaf(xi, g * w[j][i], part);
-                dw[j][i] = fmaf(g, xi, dw[j][i]);
+                // (the normalised row as one value in both sums, and again below, would be kept: 18 to 48 registers too many at 16384 columns)
+                const float xi = (float)x[j].v[i], g = (float)dy[j].v[i];
+                part = fmaf(xi * rstd, g * w[j][i], part);
+                dw[j][i] = fmaf(g * rstd, xi, dw[j][i]);
             }
             dot += part;
         }
