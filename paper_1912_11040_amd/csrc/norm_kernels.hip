@@ -60,6 +60,7 @@ __global__ __launch_bounds__(kThreads<TPR>) void norm_kernel(NormArgs a) {
     const int width = a.cfg.q_block && a.cfg.q_block < kVec * TPR ? a.cfg.q_block : dim;      // columns of a block; no block ends inside a lane's eight
     const bool whole = width >= dim;
     const int n_blocks = a.cfg.q_block ? (dim + a.cfg.q_block - 1) / a.cfg.q_block : 1;
+    const float least = a.cfg.eps < 0x1p-120f ? 0x1p-100f : 0.f;      // of a sum of squares that nothing is lost of next to eps
     float w[NV][kVec];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -91,9 +92,9 @@ __global__ __launch_bounds__(kThreads<TPR>) void norm_kernel(NormArgs a) {
         }
         float total = row_sum<TPR>(squares(s), exchange), eps = a.cfg.eps;
         int e = 0;
-        // Squares out of the range of 32 bits, where the row's values are not and eps does not outweigh what is lost: the row is divided by a
-        // power of two first, of its largest value or of eps' root.  (Nothing helps a row that holds a NaN or an infinity.)
-        if (!(total <= 3.4e38f) || (total < 0x1p-100f && eps < 0x1p-120f)) {
+        // Squares out of the range of 32 bits (or NaN), where the row's values are not and eps does not outweigh what is lost: the row is divided
+        // by a power of two first, of its largest value or of eps' root.  (Nothing helps a row that holds a NaN or an infinity.)
+        if (__builtin_expect(__builtin_amdgcn_fmed3f(total, least, 3.4e38f) != total, 0)) {
             unsigned most = 0;
 #pragma unroll
             for (int j = 0; j < NV; ++j)
@@ -149,10 +150,12 @@ __global__ __launch_bounds__(kThreads<TPR>) void norm_kernel(NormArgs a) {
             const int c = (j * TPR + lane) * kVec;
             if (!whole) most[j] = lanes_max(most[j], width / kVec);
             float scale = __uint_as_float(most[j]) / 448.f;
-            // (below the normal numbers a quotient rounded down may leave y / scale beyond e4m3's largest number: rounded up there)
-            if (scale < 0x1p-126f && scale * 448.f < __uint_as_float(most[j])) scale = __uint_as_float(__float_as_uint(scale) + 1);
+            float by = scale;
+            if (__builtin_expect(scale < 0x1p-126f, 0)) {      // not a normal number: rounded down, y / scale may be beyond e4m3's largest
+                if (scale * 448.f < __uint_as_float(most[j])) scale = __uint_as_float(__float_as_uint(scale) + 1);
+                by = scale == 0.f ? 1.f : scale;
+            }
             if (c < dim && (whole ? c == 0 : c % width == 0)) a.scale[r * n_blocks + (whole ? 0 : c / width)] = scale;
-            const float by = scale == 0.f ? 1.f : scale;
             Pack<unsigned, 2> out;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
