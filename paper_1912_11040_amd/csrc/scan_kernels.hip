@@ -27,9 +27,10 @@ __device__ inline float rate2(float a) {
 // ---- rows of sequences ----
 //
 //   h = exp(step a) h + step u b,   y = (sum c h + skip u) z sigmoid(z)
-// A state's row is a product, an exponential (four issue slots), a product and two multiply-adds: at sixteen states 128 slots a
-// (row, channel) against 8 bytes of 16-bit rows, so vector issue bounds it (64 utterances of 98 to 1598 rows, 1024 channels, bf16: 240 us, with vector
-// instructions under way all the time that its compute units are busy; their bytes would take 97 us at the rate of a copy).
+// A state's row is a product, an exponential (of the time of two), a product and two multiply-adds: at sixteen states 96 slots a
+// (row, channel) against 8 bytes of 16-bit rows, so vector issue bounds it (64 utterances of 98 to 1598 rows, 1024 channels, bf16: 235 us, with vector
+// instructions under way all the time that its compute units are busy; these five alone take 159 at the rates that they reach by
+// themselves, the bytes 97 at the rate of a copy).
 // A group of four wavefronts takes 256 / LN channels through a block of rows; LN neighbouring lanes share a channel, K states each
 // in registers, and add up their part of the output.  (A lane per channel would need no sums and a quarter of the groups; the chip is
 // hard to fill as it is.)  Rows come in tiles of TT: all lanes turn EPT elements each of u and delta into steps and step u in LDS, once
