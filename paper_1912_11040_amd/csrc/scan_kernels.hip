@@ -316,7 +316,7 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, int n_seq, i
 // walks a block forward for its states and back for its gradients, in stretches of SUB rows whose states and decays stay in registers.
 // Both are bound by vector issue: 32 utterances of 98 to 1598 rows, 1024 channels, 16 states, bf16 take 155 us (vector instructions under way 93 % of
 // the time) and 440 (87 %), the join between them 51 (HBM), the sums over tiles and runs 19, 665 in all.  In blocks of 32 rows the sums are 8 of the 30 bytes moved a (row, channel); stretches of 16
-// rows need more registers than two wavefronts per SIMD leave (1250 us with one).  So do, by 14 to 22 registers, which the compiler keeps in
+// rows need more registers than two wavefronts per SIMD leave (1250 us with one).  So do, by 15 to 21 registers, which the compiler keeps in
 // scratch, stretches of eight rows at four states a lane where a partial tile's accesses or 32-bit elements come on top; 16-bit ones of
 // whole tiles do without.
 template <int LN, int K> struct BackTile {
@@ -441,7 +441,7 @@ __global__ __launch_bounds__(256) void scan_back_sums_kernel(ScanArgs a, BackWs 
         }
     }
     // Decays that grow, by a rate above zero or a step below it, may take the product out of the range of 32 bits where no term is: the
-    // sum is then formed row by row from the last, as the definition does, and a term of zero stays zero.
+    // sum is then formed row by row from the last, as the definition does, and a term of zero stays zero (but for a decay of NaN).
     bool lost = false;
 #pragma unroll
     for (int k = 0; k < K; ++k) lost = lost || !(q[k] <= 3.4e38f);
@@ -459,7 +459,10 @@ __global__ __launch_bounds__(256) void scan_back_sums_kernel(ScanArgs a, BackWs 
 #pragma unroll 1
         for (int t = here - 1; t >= 0; --t) {
 #pragma unroll
-            for (int k = 0; k < K; ++k) back[k] = pass_block<false>(fmaf(sc[t][nq + k], sdp[t][ch], back[k]), 0.f, su[t][ch].x, rate[k]);
+            for (int k = 0; k < K; ++k) {
+                const float e = __builtin_amdgcn_exp2f(su[t][ch].x * rate[k]), g = fmaf(sc[t][nq + k], sdp[t][ch], back[k]);
+                back[k] = g == 0.f && e == e ? 0.f : e * g;
+            }
         }
     }
 #pragma unroll

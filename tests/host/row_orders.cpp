@@ -72,7 +72,7 @@ int main() {
         const int rc = aug_scan_batch(ctx, (int)off.size() - 1, off.data(), nullptr, &c, &in, nullptr, nullptr, &y);
         if (rc != AUG_OK) { ++g_faults; printf("%s\n", aug_last_error(ctx)); }
     };
-    for (int round = 0; round < 3; ++round)
+    for (int turn = 0; turn < 3; ++turn)
         for (const auto* off : {&a, &b}) {
             for (int abreast : {3, 2, 1, 100, 3, 2, 8, 100}) {
                 scan(*off, abreast);

@@ -327,3 +327,24 @@ def test_gradients_with_steps_of_both_signs(aug, lengths, dim, n, g, name):
     for k, v in _gradients(aug, off, t, dy, g, state, softplus=False).items():
         over = sum(lengths) if k in ("da", "dskip", "ddelta_bias") else dim // g if k in ("db", "dc") else 0
         agrees(v, want[k], mag[k], 2 * terms + over, k)
+
+
+@pytest.mark.parametrize("n", [3, 11, 16, 64, 128])
+@pytest.mark.parametrize("value", [float("nan"), 1e30])
+def test_gradients_behind_a_step_that_is_no_number(aug, value, n):
+    """A step of NaN makes NaN of its channel's gradients in every row before it, also where no gradient comes from behind; a step that forgets the state makes
+    zeros of what comes from behind."""
+    dim = 20
+    off, _, t, state, dy = S._inputs([150, 9], dim, n, 1, torch.float32, 110 + n)
+    dy[60:150] = 0
+    t["delta"][100, 7] = value
+    args = dict(state_in=wide(state), **_wide(t))
+    with np.errstate(all="ignore"):
+        want, mag = (R.scan_backward(off, dy=wide(dy), magnitude=m, **args) for m in (False, True))
+    assert np.isnan(want["du"][:101, 7]).all() == np.isnan(value)
+    got = _gradients(aug, off, t, dy, 1, state)
+    for k in ("du", "ddelta"):
+        ref, bound, g = want[k].copy(), mag[k].copy(), wide(got[k]).copy()
+        for v in (ref, bound, g):
+            v[100:150, 7] = 1.0                           # (there and behind it the states are beyond 32 bits, or NaN)
+        agrees(torch.from_numpy(g).float(), ref, bound, 2 * S._terms([150], n), k)
