@@ -93,7 +93,8 @@ __global__ __launch_bounds__(kThreads<TPR>) void norm_kernel(NormArgs a) {
         float total = row_sum<TPR>(squares(s), exchange), eps = a.cfg.eps;
         int e = 0;
         // Squares out of the range of 32 bits (or NaN), where the row's values are not and eps does not outweigh what is lost: the row is divided
-        // by a power of two first, of its largest value or of eps' root.  (Nothing helps a row that holds a NaN or an infinity.)
+        // by a power of two first, of its largest value or of eps' root.  (Nothing helps a row that holds a NaN or an infinity.)  The question costs
+        // 16-bit rows 2 % (64 utterances of 2048 columns into 8 bits 152.6 us without it, 155.5 with), 32-bit ones nothing.
         if (__builtin_expect(__builtin_amdgcn_fmed3f(total, least, 3.4e38f) != total, 0)) {
             unsigned most = 0;
 #pragma unroll
